@@ -448,6 +448,149 @@ nm_status nm_resnet50_forward_host_async(nm_ctx* ctx, const nm_conv_params* conv
 nm_status nm_encoder_layer_static(nm_ctx* ctx, const nm_encoder_weights* w, const nm_encoder_cfg* cfg,
                                   const void* x, void* y, void* stream);
 
+/* ---------------------------------------------------------------- answering token by token
+ * A decoder that keeps its keys and values in pages runs, per layer and step,
+ *     nm_kv_plan (once per step), nm_linear_pwl[_w4], nm_qk_norm_rope_pwl, nm_attention_pwl_paged, nm_linear_pwl[_w4].
+ * (The paper evaluates encoders; these are the operators that the same method, linear operators and PWL tables, needs for
+ * one new token per sequence.)
+ * A cache is num_pages pages of page_size tokens; element (page, token, head, channel) of K and of V is at
+ * base[page*stride_page + token*stride_token + head*stride_head + channel].  A slot number is page*page_size + token.
+ * Page and slot numbers are checked on the device: one that lies outside the cache is never followed.  The kernel then leaves
+ * out the access, records NM_ERR_INVALID_ARG in the status word and goes on; what the request or token gets is not meaningful. */
+
+/* Block tables and slot maps from request lengths.  For every request i, in order:
+ *   new_tokens[i] < 0: the request is over.  Its ceil(lengths[i]/page_size) pages go back on the stack of free pages, the first
+ *     entry of its table row first; its new length is 0.
+ *   else it grows by new_tokens[i] tokens to lengths[i] + new_tokens[i]; its table row gets the pages it lacks.
+ * All released pages are pushed before the first is taken; pages are taken from the top of the stack (free_pages[0 ..
+ * free_count-1], the last one first), by request and then by table entry.
+ *   lengths_out[i], *free_count_out   the new lengths and the new height of the stack (may be the same arrays as the inputs)
+ *   block_tables [B, max_pages], pitch ld_tables; free_pages [free_capacity]: updated in place
+ *   token_start[0..B]   first new token of each request in the order of the requests; token_start[B] is their number
+ *   slots[t], positions[t], 0 <= t < max_tokens: slot and position of new token t (token j of request i has position
+ *     lengths[i] + j); behind the last new token slots are -1 and positions 0
+ * All are device int32 arrays.  A step that cannot be made changes nothing: lengths_out and free_count_out are copies, tables
+ * and free_pages stay, all of token_start and positions is 0, all slots are -1, and the status word gets NM_ERR_WORKSPACE (too
+ * few free pages), NM_ERR_SHAPE (a request longer than max_pages pages, more than max_tokens new tokens) or
+ * NM_ERR_INVALID_ARG (a negative length, one of more than max_pages pages, a free_count or a released stack outside
+ * [0, free_capacity]), the last named first where several hold. */
+typedef struct {
+    int32_t B, page_size, max_pages, max_tokens, free_capacity;
+    const int32_t* lengths;
+    const int32_t* new_tokens;
+    const int32_t* free_count;
+    int32_t* block_tables;
+    int64_t ld_tables;
+    int32_t* free_pages;
+    int32_t* lengths_out;
+    int32_t* free_count_out;
+    int32_t* token_start;
+    int32_t* slots;
+    int32_t* positions;
+} nm_kv_plan_desc;
+
+nm_status nm_kv_plan(nm_ctx* ctx, const nm_kv_plan_desc* desc, void* stream);
+
+/* Norm of every head of the queries and keys with PWL reciprocal square root, the rotation by position, and the write of keys
+ * and values to the cache, one pass over the projection.  Per token t and head:
+ *     x' = x * PWL_rsqrt(mean(x^2) + eps) * gamma            (left out for queries / keys whose gamma is NULL)
+ *     (a, b) -> (a*c - b*s, b*c + a*s)   for the rot/2 channel pairs, c = cos_sin[p][i], s = cos_sin[p][rot/2 + i], p = positions[t]
+ * Pair i is channels (i, i + rot/2), or (2i, 2i + 1) with pairs != 0; channels from rot on are not rotated (rot = 0: none are).
+ * qkv [T, (heads + 2 kv_heads)*d], pitch ld_qkv: Q | K | V as nm_linear_pwl leaves them.  q_out [T, heads*d], pitch ld_q; it
+ * may be the Q part of qkv itself.  k_out [T, kv_heads*d], pitch ld_k, or NULL: the finished keys once more (it may be the K
+ * part of qkv).  k_cache, v_cache (both or neither) and slots[t]: where the keys and values of token t go.
+ * A token whose slot is negative is padding: nothing is written for it.  Without caches slots may be NULL.
+ * positions: device int32[T], needed where rot > 0; a position outside [0, max_position) is recorded as NM_ERR_INVALID_ARG in
+ * the status word and the token treated as padding.  Two tokens of one call must not have the same slot.
+ * dtype F32, BF16 or F16 (caches likewise), fp32 inside, one rounding at the end.  d a multiple of 8, at most 256; rot even,
+ * at most d (a multiple of 16 without pairs, of 8 with them).  Pointers 16-byte aligned, all strides multiples of 16 bytes;
+ * cos_sin: device float [max_position, rot]; gamma_q, gamma_k: device float[d]. */
+typedef struct {
+    int32_t T, heads, kv_heads, d, rot, pairs;
+    nm_dtype dtype;
+    const void* qkv;
+    int64_t ld_qkv;
+    const int32_t* positions;
+    const float* cos_sin;
+    int32_t max_position;
+    const float* gamma_q;
+    const float* gamma_k;
+    float eps;
+    int32_t rsqrt_slot;
+    void* q_out;
+    int64_t ld_q;
+    void* k_out;
+    int64_t ld_k;
+    void* k_cache;
+    void* v_cache;
+    const int32_t* slots;
+    int32_t num_pages, page_size;
+    int64_t stride_page, stride_token, stride_head;
+} nm_qk_rope_desc;
+
+nm_status nm_qk_norm_rope_pwl(nm_ctx* ctx, const nm_qk_rope_desc* desc, void* stream);
+
+/* Attention of one new token per request over the paged cache, PWL softmax as in nm_attention_pwl.  Per request b and head h,
+ * over the lengths[b] tokens that its pages hold (head h reads key head h / (heads / kv_heads)):
+ *     s_j = scale * <q, k_j>;  m = max_j s_j;  e_j = PWL_exp(s_j - m);  o = (sum_j e_j * v_j) * PWL_recip(sum_j e_j)
+ * m is the maximum over all of the request's tokens (a PWL exponential is not multiplicative).  A request of length 0 gets
+ * zeros.  Token j is at page block_tables[b*ld_tables + j / page_size], place j % page_size; entries and places behind the
+ * length are not read.  A length outside [0, max_len] is recorded as NM_ERR_SHAPE in the status word and the request's
+ * output left as it was.  max_len (at most max_pages*page_size) is what the launch and the workspace are sized for.
+ * Q [B, heads*d], pitch ld_q; out likewise, ld_out.  dtype F32, BF16 or F16 for Q, the caches and out; fp32 scores, sums and
+ * probabilities (the 16-bit types multiply probabilities into V as two terms, 16 bits of them for BF16, 22 for F16).
+ * heads a multiple of kv_heads; d a multiple of 8, at most 256.  Pointers 16-byte aligned, strides multiples of 16 bytes.
+ * workspace: device, 256-byte aligned, nm_attention_paged_workspace_bytes of it (0 on a bad descriptor); calls that may be in
+ * flight together, replays of captured graphs among them, need one each. */
+typedef struct {
+    int32_t B, heads, kv_heads, d;
+    nm_dtype dtype;
+    int32_t num_pages, page_size, max_pages, max_len;
+    const void* Q;
+    int64_t ld_q;
+    const void* k_cache;
+    const void* v_cache;
+    int64_t stride_page, stride_token, stride_head;
+    const int32_t* block_tables;
+    int64_t ld_tables;
+    const int32_t* lengths;
+    float scale;
+    int32_t exp_slot, recip_slot;
+    void* out;
+    int64_t ld_out;
+} nm_attn_paged_desc;
+
+size_t nm_attention_paged_workspace_bytes(const nm_attn_paged_desc* desc);
+nm_status nm_attention_pwl_paged(nm_ctx* ctx, const nm_attn_paged_desc* desc, void* workspace, size_t ws_bytes, void* stream);
+
+/* The linear operator for few tokens with 4-bit weights:
+ *     out[m][n] = PWL_slot(sum_g scales[n][g] * sum_{k in group g} (c[n][k] - 8) * A[m][k] + bias[n]) + residual[m][n]
+ * codes [N, K/2] bytes, pitch ld_codes bytes: c[n][k] in 0..15, the even k of a pair in a byte's low half.  scales [N, K/group]
+ * of A's dtype, pitch ld_scales; group 32, 64 or 128, K a multiple of it.  A [M, K], pitch lda, out and residual (or NULL) [M, N],
+ * of one dtype: F32, BF16 or F16.  bias: device float[N] or NULL; slot: NM_SLOT_NONE for no table.  Codes and 16-bit
+ * activations multiply exactly, sums are fp32.  Meant for few tokens (the weights are read once for every 32 of them); any M is taken.
+ * A, codes and out 16-byte aligned with pitches that are multiples of 16 bytes, residual likewise; scales and bias aligned
+ * to their elements. */
+typedef struct {
+    int64_t M, N, K;
+    nm_dtype dtype;
+    int32_t group;
+    const void* A;
+    int64_t lda;
+    const uint8_t* codes;
+    int64_t ld_codes;
+    const void* scales;
+    int64_t ld_scales;
+    const float* bias;
+    const void* residual;
+    int64_t ldr;
+    int32_t slot;
+    void* out;
+    int64_t ldo;
+} nm_linear_w4_desc;
+
+nm_status nm_linear_pwl_w4(nm_ctx* ctx, const nm_linear_w4_desc* desc, void* stream);
+
 /* Diagnostic for the failure-detection path (no counterpart in the paper): launches a one-warp kernel
  * that waits on a barrier nothing ever arrives on.  Like every wait in the tensor-core kernels, the
  * wait is bounded: after limit_cycles SM clock cycles (1 .. 4e9) it gives up, writes NM_ERR_TIMEOUT to
@@ -470,7 +613,8 @@ int64_t nm_ctx_launch_count(nm_ctx* ctx, int reset);
  * read plus written (one pass each way) for the bandwidth-bound row kernels. */
 enum { NM_KERNEL_PWL_APPLY = 0, NM_KERNEL_LAYERNORM = 1, NM_KERNEL_QUANTIZE = 2, NM_KERNEL_LINEAR_SIMT = 3,
        NM_KERNEL_LINEAR_TC = 4, NM_KERNEL_ATTENTION_SIMT = 5, NM_KERNEL_ATTENTION_TC = 6, NM_KERNEL_IM2COL = 7,
-       NM_KERNEL_POOL = 8, NM_NUM_KERNEL_KINDS = 9 };
+       NM_KERNEL_POOL = 8, NM_KERNEL_KV_PLAN = 9, NM_KERNEL_QK_ROPE = 10, NM_KERNEL_ATTENTION_PAGED = 11,
+       NM_KERNEL_LINEAR_W4 = 12, NM_NUM_KERNEL_KINDS = 13 };
 nm_status nm_ctx_profile_enable(nm_ctx* ctx, int on);
 nm_status nm_ctx_profile_read(nm_ctx* ctx, int kind, int64_t* launches, double* total_ms, double* total_work);
 

@@ -38,10 +38,11 @@ EXPORTS = [
     "nm_conv2d_workspace_bytes", "nm_conv2d_pwl", "nm_maxpool2d", "nm_maxpool2d_pwl", "nm_avgpool_global", "nm_resnet50_workspace_bytes",
     "nm_resnet50_forward", "nm_resnet50_forward_host", "nm_pwl_table_build_elastic",
     "nm_selftest_bounded_wait", "nm_attention_pwl_i8", "nm_encoder_stack_host_async", "nm_resnet50_forward_host_async",
-    "nm_resnet_conv_count",
+    "nm_resnet_conv_count", "nm_kv_plan", "nm_qk_norm_rope_pwl", "nm_attention_paged_workspace_bytes", "nm_attention_pwl_paged",
+    "nm_linear_pwl_w4",
 ]
 KERNEL_KINDS = ("pwl_apply", "layernorm", "quantize", "linear_simt", "linear_tc", "attention_simt", "attention_tc",
-                "im2col", "pool")
+                "im2col", "pool", "kv_plan", "qk_rope", "attention_paged", "linear_w4")
 RESNET50_CONVS = 53
 
 
@@ -103,6 +104,39 @@ class EncoderCfg(C.Structure):
     _fields_ = [("B", C.c_int32), ("L", C.c_int32), ("H", C.c_int32), ("heads", C.c_int32), ("F", C.c_int32),
                 ("dtype", C.c_int), ("eps", C.c_float), ("gelu_slot", C.c_int32), ("exp_slot", C.c_int32),
                 ("recip_slot", C.c_int32), ("rsqrt_slot", C.c_int32), ("algo", C.c_int32)]
+
+
+class KvPlanDesc(C.Structure):
+    _fields_ = [("B", C.c_int32), ("page_size", C.c_int32), ("max_pages", C.c_int32), ("max_tokens", C.c_int32),
+                ("free_capacity", C.c_int32), ("lengths", C.c_void_p), ("new_tokens", C.c_void_p), ("free_count", C.c_void_p),
+                ("block_tables", C.c_void_p), ("ld_tables", C.c_int64), ("free_pages", C.c_void_p), ("lengths_out", C.c_void_p),
+                ("free_count_out", C.c_void_p), ("token_start", C.c_void_p), ("slots", C.c_void_p), ("positions", C.c_void_p)]
+
+
+class QkRopeDesc(C.Structure):
+    _fields_ = [("T", C.c_int32), ("heads", C.c_int32), ("kv_heads", C.c_int32), ("d", C.c_int32), ("rot", C.c_int32),
+                ("pairs", C.c_int32), ("dtype", C.c_int), ("qkv", C.c_void_p), ("ld_qkv", C.c_int64), ("positions", C.c_void_p),
+                ("cos_sin", C.c_void_p), ("max_position", C.c_int32), ("gamma_q", C.c_void_p), ("gamma_k", C.c_void_p),
+                ("eps", C.c_float), ("rsqrt_slot", C.c_int32), ("q_out", C.c_void_p), ("ld_q", C.c_int64), ("k_out", C.c_void_p),
+                ("ld_k", C.c_int64), ("k_cache", C.c_void_p), ("v_cache", C.c_void_p), ("slots", C.c_void_p),
+                ("num_pages", C.c_int32), ("page_size", C.c_int32), ("stride_page", C.c_int64), ("stride_token", C.c_int64),
+                ("stride_head", C.c_int64)]
+
+
+class AttnPagedDesc(C.Structure):
+    _fields_ = [("B", C.c_int32), ("heads", C.c_int32), ("kv_heads", C.c_int32), ("d", C.c_int32), ("dtype", C.c_int),
+                ("num_pages", C.c_int32), ("page_size", C.c_int32), ("max_pages", C.c_int32), ("max_len", C.c_int32),
+                ("Q", C.c_void_p), ("ld_q", C.c_int64), ("k_cache", C.c_void_p), ("v_cache", C.c_void_p),
+                ("stride_page", C.c_int64), ("stride_token", C.c_int64), ("stride_head", C.c_int64), ("block_tables", C.c_void_p),
+                ("ld_tables", C.c_int64), ("lengths", C.c_void_p), ("scale", C.c_float), ("exp_slot", C.c_int32),
+                ("recip_slot", C.c_int32), ("out", C.c_void_p), ("ld_out", C.c_int64)]
+
+
+class LinearW4Desc(C.Structure):
+    _fields_ = [("M", C.c_int64), ("N", C.c_int64), ("K", C.c_int64), ("dtype", C.c_int), ("group", C.c_int32), ("A", C.c_void_p),
+                ("lda", C.c_int64), ("codes", C.c_void_p), ("ld_codes", C.c_int64), ("scales", C.c_void_p), ("ld_scales", C.c_int64),
+                ("bias", C.c_void_p), ("residual", C.c_void_p), ("ldr", C.c_int64), ("slot", C.c_int32), ("out", C.c_void_p),
+                ("ldo", C.c_int64)]
 
 
 _lib = None
@@ -170,6 +204,12 @@ def load():
     lib.nm_resnet50_forward_host_async.argtypes = lib.nm_resnet50_forward_host.argtypes
     lib.nm_resnet_conv_count.restype = C.c_int32
     lib.nm_resnet_conv_count.argtypes = [C.POINTER(Resnet50Cfg)]
+    lib.nm_kv_plan.argtypes = [C.c_void_p, C.POINTER(KvPlanDesc), C.c_void_p]
+    lib.nm_qk_norm_rope_pwl.argtypes = [C.c_void_p, C.POINTER(QkRopeDesc), C.c_void_p]
+    lib.nm_attention_paged_workspace_bytes.restype = C.c_size_t
+    lib.nm_attention_paged_workspace_bytes.argtypes = [C.POINTER(AttnPagedDesc)]
+    lib.nm_attention_pwl_paged.argtypes = [C.c_void_p, C.POINTER(AttnPagedDesc), C.c_void_p, C.c_size_t, C.c_void_p]
+    lib.nm_linear_pwl_w4.argtypes = [C.c_void_p, C.POINTER(LinearW4Desc), C.c_void_p]
     lib.nm_selftest_bounded_wait.argtypes = [C.c_void_p, C.c_int64, C.c_void_p]
     lib.nm_ctx_profile_enable.argtypes = [C.c_void_p, C.c_int]
     lib.nm_ctx_profile_read.argtypes = [C.c_void_p, C.c_int, C.POINTER(C.c_int64), C.POINTER(C.c_double),
@@ -205,6 +245,43 @@ def _stream(stream=None):
     torch = _torch()
     s = stream if stream is not None else torch.cuda.current_stream()
     return C.c_void_p(s.cuda_stream)
+
+
+def _want(name, t, dtype, shape, inner=True):
+    """The C calls cannot see what a pointer's tensor is: its type, extents (None: any) and contiguous rows are checked here."""
+    torch = _torch()
+    if t.dtype != dtype:
+        raise ValueError("%s: %s wanted, got %s" % (name, str(dtype).replace("torch.", ""), str(t.dtype).replace("torch.", "")))
+    if t.dim() != len(shape) or any(n is not None and n != m for n, m in zip(shape, t.shape)):
+        raise ValueError("%s: shape %s wanted, got %s" % (name, tuple("any" if n is None else n for n in shape), tuple(t.shape)))
+    if inner and t.dim() > 0 and t.shape[-1] > 1 and t.stride(-1) != 1:
+        raise ValueError("%s: the last dimension has to be contiguous" % name)
+    if t.dim() == 1 and t.shape[0] == 0:
+        return t
+    if t.device.type != "cuda" and torch.cuda.is_available():
+        raise ValueError("%s: a CUDA tensor is wanted, got one on %s" % (name, t.device))
+    return t
+
+
+def _same_device(tensors):
+    seen = {str(t.device) for t in tensors if t is not None}
+    if len(seen) > 1:
+        raise ValueError("tensors on several devices: %s" % ", ".join(sorted(seen)))
+
+
+def _pitch(t):
+    """Distance of a matrix's rows in elements; a single row has none, so its length as whole 16-byte pieces stands for it."""
+    return t.stride(0) if t.shape[0] > 1 else -(-t.shape[1] // 16) * 16
+
+
+def _cache_strides(k_cache, v_cache, dtype, kv_heads, d):
+    """[num_pages, page_size, kv_heads, d] views of any strides with contiguous channels, K's and V's alike."""
+    _want("k_cache", k_cache, dtype, (None, None, kv_heads, d))
+    _want("v_cache", v_cache, dtype, tuple(k_cache.shape))
+    if k_cache.stride()[:3] != v_cache.stride()[:3]:
+        raise ValueError("k_cache and v_cache: the same strides are wanted, got %s and %s" % (k_cache.stride(), v_cache.stride()))
+    # the stride of an extent of one is never used
+    return k_cache.shape[0], k_cache.shape[1], [s if n > 1 else 0 for s, n in zip(k_cache.stride()[:3], k_cache.shape[:3])]
 
 
 def pwl_table_build(func: int, n: int, x_min: float, x_max: float):
@@ -245,6 +322,10 @@ class Context:
             self.close()
         except Exception:
             pass
+
+    def _stream(self, stream):
+        """The given stream, or the current one of the context's device."""
+        return C.c_void_p((stream if stream is not None else _torch().cuda.current_stream(self.device)).cuda_stream)
 
     # -- tables -------------------------------------------------------------------
     def pwl_table_load(self, slot, n, x_min, x_max, k, b):
@@ -372,6 +453,139 @@ class Context:
     def quantize_i8(self, x, inv_scale, q, stream=None):
         _check(self._lib.nm_quantize_i8(self._h, _ptr(x), dtype_of(x), x.numel(), inv_scale, _ptr(q),
                                         _stream(stream)), "nm_quantize_i8")
+
+    # -- one decoding step over a paged key-value cache ------------------------------
+    # A descriptor is built once for a set of buffers and used for every step; it keeps its tensors alive.
+    @staticmethod
+    def kv_plan_desc(lengths, new_tokens, block_tables, free_pages, free_count, page_size, lengths_out, free_count_out, token_start, slots,
+                     positions):
+        """All int32 device tensors: lengths, new_tokens, lengths_out [B], block_tables [B, max_pages], free_pages
+        [capacity], free_count, free_count_out [1], token_start [B + 1], slots, positions [max_tokens]."""
+        i32 = _torch().int32
+        B = lengths.shape[0]
+        d = KvPlanDesc()
+        one_dim = {"lengths": (lengths, B), "new_tokens": (new_tokens, B), "free_pages": (free_pages, None), "free_count": (free_count, 1),
+                   "lengths_out": (lengths_out, B), "free_count_out": (free_count_out, 1), "token_start": (token_start, B + 1),
+                   "slots": (slots, None), "positions": (positions, slots.shape[0])}
+        for name, (t, n) in one_dim.items():
+            setattr(d, name, _want(name, t, i32, (n,)).data_ptr())
+        d.block_tables = _want("block_tables", block_tables, i32, (B, None)).data_ptr()
+        d.B, d.page_size, d.max_pages = B, int(page_size), block_tables.shape[1]
+        d.max_tokens, d.free_capacity, d.ld_tables = slots.shape[0], free_pages.shape[0], _pitch(block_tables) if B else d.max_pages
+        d.tensors = [t for t, _ in one_dim.values()] + [block_tables]
+        _same_device(d.tensors)
+        return d
+
+    def kv_plan(self, desc, stream=None):
+        _check(self._lib.nm_kv_plan(self._h, C.byref(desc), self._stream(stream)), "nm_kv_plan")
+
+    @staticmethod
+    def qk_rope_desc(qkv, heads, kv_heads, d, q_out, positions=None, cos_sin=None, gamma_q=None, gamma_k=None, eps=1e-6, pairs=False,
+                     k_cache=None, v_cache=None, slots=None, k_out=None, rsqrt_slot=SLOT_RSQRT):
+        """qkv [T, (heads + 2 kv_heads) d] (Q | K | V), q_out [T, heads d], k_out [T, kv_heads d]; cos_sin [max_position, rot]
+        fp32, cosines then sines; caches [num_pages, page_size, kv_heads, d]; positions, slots int32 [T]."""
+        torch = _torch()
+        a = QkRopeDesc()
+        T = qkv.shape[0]
+        _want("qkv", qkv, qkv.dtype, (None, (heads + 2 * kv_heads) * d))
+        _want("q_out", q_out, qkv.dtype, (T, heads * d))
+        a.T, a.heads, a.kv_heads, a.d, a.dtype = T, heads, kv_heads, d, dtype_of(qkv)
+        a.qkv, a.ld_qkv, a.q_out, a.ld_q = qkv.data_ptr(), _pitch(qkv), q_out.data_ptr(), _pitch(q_out)
+        if cos_sin is not None:
+            _want("cos_sin", cos_sin, torch.float32, (None, None))
+            if not cos_sin.is_contiguous():
+                raise ValueError("cos_sin: a contiguous tensor is wanted")
+            if positions is None:
+                raise ValueError("positions: wanted with cos_sin")
+            a.max_position, a.rot = cos_sin.shape
+            a.cos_sin = cos_sin.data_ptr()
+            a.positions = _want("positions", positions, torch.int32, (T,)).data_ptr()
+        for name, g in (("gamma_q", gamma_q), ("gamma_k", gamma_k)):
+            if g is not None:
+                setattr(a, name, _want(name, g, torch.float32, (d,)).data_ptr())
+        a.eps, a.rsqrt_slot, a.pairs = eps, rsqrt_slot, 1 if pairs else 0
+        if k_out is not None:
+            _want("k_out", k_out, qkv.dtype, (T, kv_heads * d))
+            a.k_out, a.ld_k = k_out.data_ptr(), _pitch(k_out)
+        if (k_cache is None) != (v_cache is None):
+            raise ValueError("k_cache and v_cache: both or neither")
+        if slots is not None:
+            a.slots = _want("slots", slots, torch.int32, (T,)).data_ptr()
+        if k_cache is not None:
+            if slots is None:
+                raise ValueError("slots: wanted with the caches")
+            a.num_pages, a.page_size, (a.stride_page, a.stride_token, a.stride_head) = _cache_strides(k_cache, v_cache, qkv.dtype, kv_heads, d)
+            a.k_cache, a.v_cache = k_cache.data_ptr(), v_cache.data_ptr()
+        a.tensors = [qkv, q_out, positions, cos_sin, gamma_q, gamma_k, k_cache, v_cache, slots, k_out]
+        _same_device(a.tensors)
+        return a
+
+    def qk_norm_rope_pwl(self, desc, stream=None):
+        _check(self._lib.nm_qk_norm_rope_pwl(self._h, C.byref(desc), self._stream(stream)), "nm_qk_norm_rope_pwl")
+
+    @staticmethod
+    def attn_paged_desc(q, k_cache, v_cache, block_tables, lengths, out, max_len=None, scale=None, exp_slot=SLOT_EXP, recip_slot=SLOT_RECIP):
+        """q, out [B, heads, d] (contiguous heads); caches [num_pages, page_size, kv_heads, d]; block_tables int32 [B, max_pages],
+        lengths int32 [B].  max_len: the longest request that the calls have to take (None: what the tables hold)."""
+        torch = _torch()
+        a = AttnPagedDesc()
+        B, heads, d = _want("q", q, q.dtype, (None, None, None)).shape
+        for name, t in (("q", q), ("out", out)):
+            _want(name, t, q.dtype, (B, heads, d))
+            if heads > 1 and t.stride(1) != d:
+                raise ValueError("%s: the heads of a request have to be contiguous" % name)
+        a.B, a.heads, a.d, a.dtype, a.kv_heads = B, heads, d, dtype_of(q), k_cache.shape[2] if k_cache.dim() == 4 else 0
+        a.num_pages, a.page_size, (a.stride_page, a.stride_token, a.stride_head) = _cache_strides(k_cache, v_cache, q.dtype, a.kv_heads, d)
+        _want("block_tables", block_tables, torch.int32, (B, None))
+        _want("lengths", lengths, torch.int32, (B,))
+        a.max_pages = block_tables.shape[1]
+        a.max_len = a.max_pages * a.page_size if max_len is None else int(max_len)
+        row = heads * d
+        a.Q, a.ld_q, a.out, a.ld_out = q.data_ptr(), q.stride(0) if B > 1 else row, out.data_ptr(), out.stride(0) if B > 1 else row
+        a.k_cache, a.v_cache = k_cache.data_ptr(), v_cache.data_ptr()
+        a.block_tables, a.ld_tables, a.lengths = block_tables.data_ptr(), _pitch(block_tables) if B else a.max_pages, lengths.data_ptr()
+        a.scale = float(scale) if scale is not None else float(d) ** -0.5
+        a.exp_slot, a.recip_slot = exp_slot, recip_slot
+        a.tensors = [q, k_cache, v_cache, block_tables, lengths, out]
+        _same_device(a.tensors)
+        return a
+
+    def attention_paged_workspace_bytes(self, desc) -> int:
+        return int(self._lib.nm_attention_paged_workspace_bytes(C.byref(desc)))
+
+    def attention_pwl_paged(self, desc, workspace=None, stream=None):
+        ws = workspace.numel() * workspace.element_size() if workspace is not None else 0
+        _check(self._lib.nm_attention_pwl_paged(self._h, C.byref(desc), _ptr(workspace), ws, self._stream(stream)), "nm_attention_pwl_paged")
+
+    @staticmethod
+    def linear_w4_desc(A, codes, scales, out, bias=None, residual=None, slot=SLOT_NONE):
+        """A [M, K]; codes uint8 [N, K/2], the even k of a pair in the low half; scales [N, K/group] of A's type; out, residual
+        [M, N]; bias fp32 [N]."""
+        torch = _torch()
+        M, K = _want("A", A, A.dtype, (None, None)).shape
+        N = codes.shape[0]
+        _want("codes", codes, torch.uint8, (N, K // 2))
+        _want("scales", scales, A.dtype, (N, None))
+        _want("out", out, A.dtype, (M, N))
+        a = LinearW4Desc()
+        groups = scales.shape[1]
+        if groups == 0 or K % groups or K % 2:
+            raise ValueError("scales: %d columns do not divide K = %d into groups" % (groups, K))
+        a.M, a.N, a.K, a.dtype, a.group = M, N, K, dtype_of(A), K // groups
+        a.A, a.lda, a.codes, a.ld_codes = A.data_ptr(), _pitch(A), codes.data_ptr(), _pitch(codes)
+        a.scales, a.ld_scales, a.out, a.ldo = scales.data_ptr(), _pitch(scales), out.data_ptr(), _pitch(out)
+        if bias is not None:
+            a.bias = _want("bias", bias, torch.float32, (N,)).data_ptr()
+        if residual is not None:
+            _want("residual", residual, A.dtype, (M, N))
+            a.residual, a.ldr = residual.data_ptr(), _pitch(residual)
+        a.slot = slot
+        a.tensors = [A, codes, scales, out, bias, residual]
+        _same_device(a.tensors)
+        return a
+
+    def linear_pwl_w4(self, desc, stream=None):
+        _check(self._lib.nm_linear_pwl_w4(self._h, C.byref(desc), self._stream(stream)), "nm_linear_pwl_w4")
 
     # -- CNN ----------------------------------------------------------------------
     @staticmethod

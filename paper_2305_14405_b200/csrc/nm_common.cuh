@@ -802,3 +802,48 @@ nm_status nm_launch_maxpool(nm_ctx* ctx, const void* x, void* y, nm_dtype dt, in
 nm_status nm_launch_avgpool(nm_ctx* ctx, const void* x, void* y, nm_dtype dt, int Nb, int HW, int C, cudaStream_t st);
 // fills the 64 x 64 matrix `w` with `value` on the diagonal and zero elsewhere
 nm_status nm_launch_fill_diag(nm_ctx* ctx, void* w, nm_dtype dt, float value, cudaStream_t st);
+
+// ---- one decoding step over a paged cache (decode_api.cu checks the arguments) ----
+// Makes the context's device the current one for a call, whatever the caller's thread has set.
+struct NmDeviceScope {
+    int before;
+    bool ok, set;
+    explicit NmDeviceScope(const nm_ctx* ctx) : before(-1), ok(cudaGetDevice(&before) == cudaSuccess), set(false)
+    {
+        if (ok && before != ctx->device) ok = set = cudaSetDevice(ctx->device) == cudaSuccess;
+    }
+    ~NmDeviceScope()
+    {
+        if (set) cudaSetDevice(before);
+    }
+};
+nm_status nm_launch_kv_plan(nm_ctx* ctx, const nm_kv_plan_desc* d, cudaStream_t st);
+nm_status nm_launch_qk_rope(nm_ctx* ctx, const nm_qk_rope_desc* d, cudaStream_t st);
+size_t nm_attention_paged_bytes(const nm_attn_paged_desc* d);   // of a checked descriptor
+nm_status nm_launch_attention_paged(nm_ctx* ctx, const nm_attn_paged_desc* d, void* workspace, cudaStream_t st);
+nm_status nm_launch_linear_w4(nm_ctx* ctx, const nm_linear_w4_desc* d, cudaStream_t st);
+
+// launch attributes of a kernel that may start while its predecessor runs (every thread of it calls nm_grid_dependency_wait
+// before it touches memory)
+struct NmLaunchConfig {
+    cudaLaunchConfig_t cfg;
+    cudaLaunchAttribute attr[2];
+    NmLaunchConfig(const nm_ctx* ctx, dim3 grid, int threads, size_t smem, cudaStream_t st, int cluster = 1) : cfg(), attr()
+    {
+        cfg.gridDim = grid;
+        cfg.blockDim = dim3(threads);
+        cfg.dynamicSmemBytes = smem;
+        cfg.stream = st;
+        cfg.attrs = attr;
+        if (ctx->pdl) {
+            attr[cfg.numAttrs].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+            attr[cfg.numAttrs++].val.programmaticStreamSerializationAllowed = 1;
+        }
+        if (cluster > 1) {
+            attr[cfg.numAttrs].id = cudaLaunchAttributeClusterDimension;
+            attr[cfg.numAttrs].val.clusterDim.x = cluster;
+            attr[cfg.numAttrs].val.clusterDim.y = attr[cfg.numAttrs].val.clusterDim.z = 1;
+            cfg.numAttrs++;
+        }
+    }
+};
