@@ -14,7 +14,10 @@
 
 namespace {
 
-constexpr int PAGED_WARPS = 8, PAGED_THREADS = PAGED_WARPS * 32;
+#ifndef RINGB
+#define RINGB 8192
+#endif
+constexpr int PAGED_WARPS = 8, PAGED_THREADS = PAGED_WARPS * 32, PAGED_RING = RINGB;   // bytes of a warp's ring
 
 struct PagedArgs {
     nm_attn_paged_desc d;
@@ -69,6 +72,40 @@ __device__ __forceinline__ void paged_offsets(const PagedArgs& a, int b, int fir
     }
 }
 
+// Asynchronous copies: a warp copies what it will read itself, so its tiles need no barrier of the block.  Invalid tokens are filled
+// with zeros.
+__device__ __forceinline__ void paged_copy(uint32_t dst, const void* src, bool valid)
+{
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(valid ? 16 : 0) : "memory");
+}
+__device__ __forceinline__ void paged_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N> __device__ __forceinline__ void paged_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+
+// Runs a warp's tiles through its ring: fetch(i0, stage) starts the copies of the tile at token i0, use(i0, stage) consumes it.  `ready` is
+// called once the first tiles are on their way.
+template <int STAGES, int TILE, typename Fetch, typename Ready, typename Use>
+__device__ __forceinline__ void paged_pipeline(int count, Fetch fetch, Ready ready, Use use)
+{
+    constexpr int STEP = PAGED_WARPS * TILE;
+    int i0 = (threadIdx.x >> 5) * TILE, next = i0, stage = 0;
+#pragma unroll
+    for (int s = 0; s < STAGES - 1; ++s, next += STEP) {
+        if (next < count) fetch(next, s);
+        paged_commit();
+    }
+    ready();
+    for (; i0 < count; i0 += STEP, next += STEP) {
+        if (next < count) fetch(next, stage == 0 ? STAGES - 1 : stage - 1);   // the stage that the tile before has left
+        paged_commit();
+        paged_wait<STAGES - 1>();
+        __syncwarp();   // the lanes' copies are there
+        use(i0, stage);
+        __syncwarp();   // and have been read
+        stage = stage == STAGES - 1 ? 0 : stage + 1;
+    }
+    paged_wait<0>();
+}
+
 // ---------------------------------------------------------------- tensor-core tiles
 
 __device__ __forceinline__ void paged_mma(float* c, uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1, __nv_bfloat16)
@@ -99,60 +136,90 @@ __device__ __forceinline__ uint32_t paged_term(float& a, float& b, __half)
     return *reinterpret_cast<const uint32_t*>(&h);
 }
 
-// Tiles of 16 tokens, NT tiles of 8 query heads.  Lane (g, t) = (lane / 4, lane % 4).
-//   scores  S^T = K Q^T: lane (g, t) loads 16 bytes of tokens g and g + 8 in every 32 channels, which four of its neighbours make 64
-//           contiguous bytes.  Which channel is which k of a product is free as long as Q has the same order.
-//   values  O^T = V^T P^T: lane (g, t) loads 8 channels of tokens 2t, 2t + 1, 2t + 8, 2t + 9 in every 64 (4 in a last 32), so rows
-//           are read 128 bytes at a time; a byte permutation pairs two tokens' channels.  Probabilities are two 16-bit terms.
+// Four 8 x 8 matrices of 16-bit numbers, lane l giving the address of row l % 8 of matrix l / 8; transposed on request.
+__device__ __forceinline__ void paged_ldmatrix(uint32_t* r, uint32_t at)
+{
+    asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0,%1,%2,%3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(at) : "memory");
+}
+__device__ __forceinline__ void paged_ldmatrix_trans(uint32_t* r, uint32_t at)
+{
+    asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3])
+                 : "r"(at)
+                 : "memory");
+}
+
+// Tiles of 16 tokens, NT tiles of 8 query heads: S^T = K Q^T and O^T = V^T P^T, tokens or channels as rows, so that eight heads fill
+// a product.  Rows are copied whole (fragments loaded from the cache directly would take 64 bytes of a row at a time: 2.9 to 4.9 TB/s
+// where whole rows reach ...) and lie in the ring with their 16-byte pieces permuted, piece c of row r at c ^ (r & 7)
+// (rows of 96 channels one piece apart instead): neither the copies nor the matrix reads collide.
+// Probabilities are two 16-bit terms.
 template <typename T, int D_, int NT> struct PagedMma {
     using Elem = T;
-    static constexpr int D = D_, HEADS = NT * 8, TILE = 16, WIDE = D / 64, NARROW = (D % 64) / 32;
-    static_assert(D % 32 == 0, "whole 32-channel pieces");
+    static constexpr int D = D_, HEADS = NT * 8, TILE = 16, LANES = D / 8;   // lanes of a row
+    static constexpr bool POW2 = (LANES & (LANES - 1)) == 0;
+    static constexpr int PITCH = D * 2 + (POW2 ? 0 : 16), STAGE = TILE * PITCH, STAGES = PAGED_RING / STAGE < 2 ? 2 : PAGED_RING / STAGE, RING = STAGES * STAGE;   // bytes of a warp
+    static_assert(D % 32 == 0 && HEADS * D * 4 <= RING, "whole 32-channel pieces; a warp's sums fit its ring");
+    static __device__ __forceinline__ float2 read(const float* s) { return *reinterpret_cast<const float2*>(s); }   // two tokens' scores
 
-    // put(h, i, s) takes the score of head h and token i; max_of(h) of the warp's scores is left in m for lane 0's readers
-    template <typename Put>
-    static __device__ __forceinline__ void scores(const PagedArgs& a, const T* Q, int nh, const T* K, const int64_t* off, int count, float* warp_max,
-                                                  Put put)
+    static __device__ __forceinline__ uint32_t piece(int row, int c) { return row * PITCH + ((POW2 ? c ^ (row & 7) : c) << 4); }
+    static __device__ __forceinline__ void fetch(const T* base, const int64_t* off, int count, uint32_t ring_at, int i0, int stage)
     {
-        const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, t = lane & 3;
-        uint4 q[NT][D / 32];
+        const int lane = threadIdx.x & 31;
 #pragma unroll
-        for (int n = 0; n < NT; ++n)
-#pragma unroll
-            for (int c = 0; c < D / 32; ++c)
-                q[n][c] = n * 8 + g < nh ? *reinterpret_cast<const uint4*>(Q + (n * 8 + g) * D + c * 32 + t * 8) : make_uint4(0, 0, 0, 0);
-        float m[NT][2];
-#pragma unroll
-        for (int n = 0; n < NT; ++n) m[n][0] = m[n][1] = -INFINITY;
-        for (int i0 = warp * TILE; i0 < count; i0 += PAGED_WARPS * TILE) {
-            const int i = i0 + g;
-            const int64_t at0 = i < count ? off[i] : -1, at1 = i + 8 < count ? off[i + 8] : -1;
-            uint4 k0[D / 32], k1[D / 32];
-#pragma unroll
-            for (int c = 0; c < D / 32; ++c) {
-                k0[c] = at0 >= 0 ? __ldg(reinterpret_cast<const uint4*>(K + at0 + c * 32 + t * 8)) : make_uint4(0, 0, 0, 0);
-                k1[c] = at1 >= 0 ? __ldg(reinterpret_cast<const uint4*>(K + at1 + c * 32 + t * 8)) : make_uint4(0, 0, 0, 0);
-            }
-            float s[NT][4];
-#pragma unroll
-            for (int n = 0; n < NT; ++n) {
-                s[n][0] = s[n][1] = s[n][2] = s[n][3] = 0.f;
-#pragma unroll
-                for (int c = 0; c < D / 32; ++c) {
-                    paged_mma(s[n], k0[c].x, k1[c].x, k0[c].y, k1[c].y, q[n][c].x, q[n][c].y, T());
-                    paged_mma(s[n], k0[c].z, k1[c].z, k0[c].w, k1[c].w, q[n][c].z, q[n][c].w, T());
-                }
-#pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    const float v = s[n][r] * a.d.scale;
-                    const int j = i + (r >> 1) * 8;
-                    if (j < count) {
-                        m[n][r & 1] = fmaxf(m[n][r & 1], v);
-                        put(n * 8 + 2 * t + (r & 1), j, v);
-                    }
-                }
-            }
+        for (int x = 0; x < TILE * LANES / 32; ++x) {
+            const int at = x * 32 + lane, row = at / LANES, c = at % LANES, i = i0 + row;
+            const int64_t o = i < count ? off[i] : -1;
+            paged_copy(ring_at + stage * STAGE + piece(row, c), o >= 0 ? base + o + c * 8 : base, o >= 0);
         }
+    }
+
+    // put(h, i, s) takes the score of head h and token i; the heads' maxima over the warp's tokens go to warp_max
+    template <typename Put>
+    static __device__ __forceinline__ void scores(const PagedArgs& a, const T* Q, int nh, const T* K, const int64_t* off, int count, unsigned char* ring,
+                                                  float* warp_max, Put put)
+    {
+        const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
+        const uint32_t ring_at = nm_smem_u32(ring);
+        uint32_t q[NT][D / 16][2];
+        float m[NT][2];
+        paged_pipeline<STAGES, TILE>(
+            count, [&](int i0, int stage) { fetch(K, off, count, ring_at, i0, stage); },
+            [&] {
+#pragma unroll
+                for (int n = 0; n < NT; ++n) {
+                    m[n][0] = m[n][1] = -INFINITY;
+#pragma unroll
+                    for (int c = 0; c < D / 16; ++c)
+#pragma unroll
+                        for (int r = 0; r < 2; ++r)
+                            q[n][c][r] = n * 8 + g < nh ? *reinterpret_cast<const uint32_t*>(Q + (n * 8 + g) * D + c * 16 + r * 8 + t * 2) : 0;
+                }
+            },
+            [&](int i0, int stage) {
+                float s[NT][4];
+#pragma unroll
+                for (int n = 0; n < NT; ++n) s[n][0] = s[n][1] = s[n][2] = s[n][3] = 0.f;
+                const uint32_t tile = ring_at + stage * STAGE;
+#pragma unroll
+                for (int c = 0; c < D / 16; ++c) {
+                    uint32_t k[4];
+                    paged_ldmatrix(k, tile + piece(lane & 15, 2 * c + (lane >> 4)));
+#pragma unroll
+                    for (int n = 0; n < NT; ++n) paged_mma(s[n], k[0], k[1], k[2], k[3], q[n][c][0], q[n][c][1], T());
+                }
+#pragma unroll
+                for (int n = 0; n < NT; ++n)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) {
+                        const float v = s[n][r] * a.d.scale;
+                        const int j = i0 + g + (r >> 1) * 8;
+                        if (j < count) {
+                            m[n][r & 1] = fmaxf(m[n][r & 1], v);
+                            put(n * 8 + 2 * t + (r & 1), j, v);
+                        }
+                    }
+            });
 #pragma unroll
         for (int n = 0; n < NT; ++n)
 #pragma unroll
@@ -163,80 +230,58 @@ template <typename T, int D_, int NT> struct PagedMma {
             }
     }
 
-    uint4 w0[WIDE ? WIDE : 1][4];   // values of tokens 2t, 2t + 1, 2t + 8, 2t + 9
-    uint2 w1[4];
-    __device__ __forceinline__ void load(const T* V, const int64_t* off, int i0, int count)
+    // get(h, i) reads the scores of head h and tokens i, i + 1; `maxima` is called once the first tiles are on their way.  The warp's
+    // sums go to warp_sum and, as [head][channel], to the ring.
+    template <typename Max, typename Get>
+    static __device__ __forceinline__ void values(const PagedArgs& a, int nh, const T* V, const int64_t* off, int count, PagedExp exp, unsigned char* ring,
+                                                  float* warp_sum, Max maxima, Get get)
     {
         const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-            const int i = i0 + 2 * t + (r & 1) + (r >> 1) * 8;
-            const int64_t at = i < count ? off[i] : -1;
-#pragma unroll
-            for (int c = 0; c < WIDE; ++c)
-                w0[c][r] = at >= 0 ? __ldg(reinterpret_cast<const uint4*>(V + at + c * 64 + g * 8)) : make_uint4(0, 0, 0, 0);
-            if (NARROW) w1[r] = at >= 0 ? __ldg(reinterpret_cast<const uint2*>(V + at + WIDE * 64 + g * 4)) : make_uint2(0, 0);
-        }
-    }
-    // get(h, i) gives the scores of head h and tokens i, i + 1; `first` is called once the first tile is on its way and gives the maxima
-    template <typename Max, typename Get>
-    __device__ __forceinline__ void values(const PagedArgs& a, int nh, const T* V, const int64_t* off, int count, PagedExp exp, float* warp_sum,
-                                           float* warp_out, Max first, Get get)
-    {
-        const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, t = lane & 3;
+        const uint32_t ring_at = nm_smem_u32(ring);
         float acc[NT][D / 16][4], sum[NT], m[NT];
-#pragma unroll
-        for (int n = 0; n < NT; ++n) {
-            sum[n] = 0.f;
-#pragma unroll
-            for (int c = 0; c < D / 16; ++c) acc[n][c][0] = acc[n][c][1] = acc[n][c][2] = acc[n][c][3] = 0.f;
-        }
-        int i0 = warp * TILE;
-        if (i0 < count) load(V, off, i0, count);
-        const float* maxima = first();
-#pragma unroll
-        for (int n = 0; n < NT; ++n) m[n] = maxima[n * 8 + g];
-        while (i0 < count) {
-            uint32_t hi[NT][2], lo[NT][2];
-#pragma unroll
-            for (int n = 0; n < NT; ++n)
-#pragma unroll
-                for (int r = 0; r < 2; ++r) {
-                    const int i = i0 + 2 * t + r * 8;
-                    float x = 0.f, y = 0.f;
-                    if (n * 8 + g < nh && i < count) {
-                        const float2 s = get(n * 8 + g, i);   // a row's storage has whole tiles
-                        x = exp(s.x - m[n]);
-                        y = i + 1 < count ? exp(s.y - m[n]) : 0.f;
-                    }
-                    sum[n] += x + y;
-                    hi[n][r] = paged_term(x, y, T());
-                    lo[n][r] = paged_term(x, y, T());
-                }
-            auto pair = [&](int c, uint32_t x0, uint32_t x1, uint32_t x8, uint32_t x9) {   // two channels of four tokens
-                const uint32_t f0 = __byte_perm(x0, x1, 0x5410), f1 = __byte_perm(x0, x1, 0x7632), f2 = __byte_perm(x8, x9, 0x5410),
-                               f3 = __byte_perm(x8, x9, 0x7632);
+        paged_pipeline<STAGES, TILE>(
+            count, [&](int i0, int stage) { fetch(V, off, count, ring_at, i0, stage); },
+            [&] {
+                const float* x = maxima();
 #pragma unroll
                 for (int n = 0; n < NT; ++n) {
-                    paged_mma(acc[n][c], f0, f1, f2, f3, hi[n][0], hi[n][1], T());
-                    paged_mma(acc[n][c], f0, f1, f2, f3, lo[n][0], lo[n][1], T());
-                }
-            };
+                    m[n] = x[n * 8 + g];
+                    sum[n] = 0.f;
 #pragma unroll
-            for (int c = 0; c < WIDE; ++c) {
-                pair(c * 4 + 0, w0[c][0].x, w0[c][1].x, w0[c][2].x, w0[c][3].x);
-                pair(c * 4 + 1, w0[c][0].y, w0[c][1].y, w0[c][2].y, w0[c][3].y);
-                pair(c * 4 + 2, w0[c][0].z, w0[c][1].z, w0[c][2].z, w0[c][3].z);
-                pair(c * 4 + 3, w0[c][0].w, w0[c][1].w, w0[c][2].w, w0[c][3].w);
-            }
-            if constexpr (NARROW != 0) {
-                pair(WIDE * 4 + 0, w1[0].x, w1[1].x, w1[2].x, w1[3].x);
-                pair(WIDE * 4 + 1, w1[0].y, w1[1].y, w1[2].y, w1[3].y);
-            }
-            i0 += PAGED_WARPS * TILE;
-            if (i0 < count) load(V, off, i0, count);
-        }
-        __syncthreads();   // scores and offsets have been read: warp_out may lie over them
+                    for (int c = 0; c < D / 16; ++c) acc[n][c][0] = acc[n][c][1] = acc[n][c][2] = acc[n][c][3] = 0.f;
+                }
+            },
+            [&](int i0, int stage) {
+                uint32_t hi[NT][2], lo[NT][2];
+#pragma unroll
+                for (int n = 0; n < NT; ++n)
+#pragma unroll
+                    for (int r = 0; r < 2; ++r) {
+                        const int i = i0 + 2 * t + r * 8;
+                        float x = 0.f, y = 0.f;
+                        if (n * 8 + g < nh && i < count) {
+                            const float2 s = get(n * 8 + g, i);   // a row's storage has whole tiles
+                            x = exp(s.x - m[n]);
+                            y = i + 1 < count ? exp(s.y - m[n]) : 0.f;
+                        }
+                        sum[n] += x + y;
+                        hi[n][r] = paged_term(x, y, T());
+                        lo[n][r] = paged_term(x, y, T());
+                    }
+                const uint32_t tile = ring_at + stage * STAGE;
+#pragma unroll
+                for (int c = 0; c < D / 16; ++c) {
+                    uint32_t v[4];   // channels c * 16 + 0..7 and 8..15 of tokens 0..7, then of tokens 8..15
+                    paged_ldmatrix_trans(v, tile + piece((lane & 7) + (lane >> 4) * 8, 2 * c + ((lane >> 3) & 1)));
+#pragma unroll
+                    for (int n = 0; n < NT; ++n) {
+                        paged_mma(acc[n][c], v[0], v[1], v[2], v[3], hi[n][0], hi[n][1], T());
+                        paged_mma(acc[n][c], v[0], v[1], v[2], v[3], lo[n][0], lo[n][1], T());
+                    }
+                }
+            });
+        __syncwarp();   // the ring has been read
+        float* out = reinterpret_cast<float*>(ring);
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
             sum[n] += __shfl_xor_sync(0xffffffffu, sum[n], 1);
@@ -245,10 +290,7 @@ template <typename T, int D_, int NT> struct PagedMma {
 #pragma unroll
             for (int c = 0; c < D / 16; ++c)
 #pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    const int ch = (c < WIDE * 4 ? (c >> 2) * 64 + g * 8 + (c & 3) * 2 : WIDE * 64 + g * 4 + (c - WIDE * 4) * 2) + (r >> 1);
-                    warp_out[(n * 8 + 2 * t + (r & 1)) * D + ch] = acc[n][c][r];
-                }
+                for (int r = 0; r < 4; ++r) out[(n * 8 + 2 * t + (r & 1)) * D + c * 16 + g + (r >> 1) * 8] = acc[n][c][r];
         }
     }
 };
@@ -266,131 +308,209 @@ template <typename T> struct Vec16 {
     }
 };
 
-// LPK lanes hold a token, VPL vectors of 16 bytes each (lanes behind the head's channels hold none): 32/LPK tokens at a time
-// against HB query heads in registers.
-template <typename T, int LPK, int VPL, int HB> struct PagedFma {
-    using Elem = T;
-    static constexpr int N = Vec16<T>::N, TILE = 32 / LPK, HEADS = HB, D = LPK * VPL * N;   // D: room for the channels
-
-    template <typename Put>
-    static __device__ __forceinline__ void scores(const PagedArgs& a, const T* Q, int nh, const T* K, const int64_t* off, int count, float* warp_max,
-                                                  Put put)
+// Sums each of v[0..COUNT-1] over the LPK lanes of a token; lane `part` of them is left with sum number first(part) .. + LEFT - 1 in
+// v[0..LEFT-1].  While there are several sums a step halves their number (each lane passes on the half that the other lane keeps),
+// so COUNT sums take COUNT - 1 shuffles, not COUNT * log2(LPK).
+template <int COUNT, int LPK> struct PagedSums {
+    static constexpr int LEFT = COUNT > LPK ? COUNT / LPK : 1;
+    static __device__ __forceinline__ void reduce(float* v, int part)
     {
-        const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, part = lane & (LPK - 1), sub = lane / LPK;
-        float q[HB][VPL][N], m[HB];
+        int n = COUNT;
 #pragma unroll
-        for (int h = 0; h < HB; ++h) {
-            m[h] = -INFINITY;
+        for (int o = LPK / 2; o > 0; o >>= 1) {
+            if (n > 1) {
+                n >>= 1;
+                const bool upper = part & o;
 #pragma unroll
-            for (int v = 0; v < VPL; ++v) {
-                const int c = (v * LPK + part) * N;
-                Vec16<T> x;
-                x.raw = h < nh && c < a.d.d ? *reinterpret_cast<const uint4*>(Q + h * a.d.d + c) : make_uint4(0, 0, 0, 0);
-                x.get(q[h][v]);
+                for (int i = 0; i < COUNT / 2; ++i)
+                    if (i < n) {
+                        const float keep = upper ? v[i + n] : v[i], give = upper ? v[i] : v[i + n];
+                        v[i] = keep + __shfl_xor_sync(0xffffffffu, give, o);
+                    }
+            } else {
+                v[0] += __shfl_xor_sync(0xffffffffu, v[0], o);
             }
         }
-        for (int i0 = warp * TILE; i0 < count; i0 += PAGED_WARPS * TILE) {
-            const int i = i0 + sub;
-            const int64_t at = i < count ? off[i] : -1;
-            float dot[HB];
+    }
+    // number of the first sum that lane `part` has
+    static __device__ __forceinline__ int first(int part)
+    {
+        int at = 0, n = COUNT;
 #pragma unroll
-            for (int h = 0; h < HB; ++h) dot[h] = 0.f;
+        for (int o = LPK / 2; o > 0; o >>= 1)
+            if (n > 1) {
+                n >>= 1;
+                at += part & o ? n : 0;
+            }
+        return at;
+    }
+    // whether the lane is the one of those with the same sums that writes them
+    static __device__ __forceinline__ bool writes(int part) { return COUNT >= LPK || (part & (LPK / COUNT - 1)) == 0; }
+};
+
+// LPK lanes hold a token, VPL vectors of 16 bytes each (lanes behind the head's channels hold none), U tokens one after another:
+// tiles of U * 32/LPK tokens against HB query heads in registers.
+template <typename T, int LPK, int VPL, int HB> struct PagedFma {
+    using Elem = T;
+    static constexpr int N = Vec16<T>::N, U = 4, SUB = 32 / LPK, TILE = U * SUB, HEADS = HB, D = LPK * VPL * N;   // D: room for the channels
+    static constexpr int STAGE = U * VPL * 512, STAGES = PAGED_RING / STAGE, RING = STAGES * STAGE;
+    static_assert(HEADS * D * 4 <= RING, "a warp's sums fit its ring");
+    static __device__ __forceinline__ float read(const float* s) { return *s; }
+
+    static __device__ __forceinline__ void fetch(const PagedArgs& a, const T* base, const int64_t* off, int count, uint32_t ring_at, int i0, int stage)
+    {
+        const int lane = threadIdx.x & 31, part = lane & (LPK - 1), sub = lane / LPK;
+#pragma unroll
+        for (int k = 0; k < U; ++k) {
+            const int i = i0 + k * SUB + sub;
+            const int64_t at = i < count ? off[i] : -1;
 #pragma unroll
             for (int v = 0; v < VPL; ++v) {
                 const int c = (v * LPK + part) * N;
-                Vec16<T> x;
-                x.raw = at >= 0 && c < a.d.d ? __ldg(reinterpret_cast<const uint4*>(K + at + c)) : make_uint4(0, 0, 0, 0);
-                float k[N];
-                x.get(k);
+                const bool valid = at >= 0 && c < a.d.d;
+                paged_copy(ring_at + stage * STAGE + (k * VPL + v) * 512 + lane * 16, valid ? base + at + c : base, valid);
+            }
+        }
+    }
+
+    template <typename Put>
+    static __device__ __forceinline__ void scores(const PagedArgs& a, const T* Q, int nh, const T* K, const int64_t* off, int count, unsigned char* ring,
+                                                  float* warp_max, Put put)
+    {
+        using Sums = PagedSums<HB * U, LPK>;   // sum number k * HB + h: token k, head h
+        const int lane = threadIdx.x & 31, part = lane & (LPK - 1), sub = lane / LPK;
+        const uint32_t ring_at = nm_smem_u32(ring);
+        const int sum0 = Sums::first(part);
+        float q[HB][VPL][N], m[Sums::LEFT];
+        paged_pipeline<STAGES, TILE>(
+            count, [&](int i0, int stage) { fetch(a, K, off, count, ring_at, i0, stage); },
+            [&] {
 #pragma unroll
                 for (int h = 0; h < HB; ++h)
 #pragma unroll
-                    for (int e = 0; e < N; ++e) dot[h] = __fmaf_rn(q[h][v][e], k[e], dot[h]);
-            }
+                    for (int v = 0; v < VPL; ++v) {
+                        const int c = (v * LPK + part) * N;
+                        Vec16<T> x;
+                        x.raw = h < nh && c < a.d.d ? *reinterpret_cast<const uint4*>(Q + h * a.d.d + c) : make_uint4(0, 0, 0, 0);
+                        x.get(q[h][v]);
+                    }
 #pragma unroll
-            for (int h = 0; h < HB; ++h)
+                for (int i = 0; i < Sums::LEFT; ++i) m[i] = -INFINITY;
+            },
+            [&](int i0, int stage) {
+                const uint4* tile = reinterpret_cast<const uint4*>(ring + stage * STAGE) + lane;
+                float dot[HB * U];
 #pragma unroll
-                for (int o = LPK / 2; o > 0; o >>= 1) dot[h] += __shfl_xor_sync(0xffffffffu, dot[h], o);
-            if (i < count) {
+                for (int k = 0; k < U; ++k) {
 #pragma unroll
-                for (int h = 0; h < HB; ++h) {
-                    const float s = dot[h] * a.d.scale;
-                    m[h] = fmaxf(m[h], s);
-                    if (part == 0 && h < nh) put(h, i, s);
+                    for (int h = 0; h < HB; ++h) dot[k * HB + h] = 0.f;
+#pragma unroll
+                    for (int v = 0; v < VPL; ++v) {
+                        Vec16<T> x;
+                        x.raw = tile[(k * VPL + v) * 32];
+                        float f[N];
+                        x.get(f);
+#pragma unroll
+                        for (int h = 0; h < HB; ++h)
+#pragma unroll
+                            for (int e = 0; e < N; ++e) dot[k * HB + h] = __fmaf_rn(q[h][v][e], f[e], dot[k * HB + h]);
+                    }
                 }
-            }
-        }
+                Sums::reduce(dot, part);
+#pragma unroll
+                for (int l = 0; l < Sums::LEFT; ++l) {
+                    const int h = (sum0 + l) % HB, i = i0 + (sum0 + l) / HB * SUB + sub;
+                    const float s = dot[l] * a.d.scale;
+                    if (i < count && h < nh) {
+                        m[l] = fmaxf(m[l], s);
+                        if (Sums::writes(part)) put(h, i, s);
+                    }
+                }
+            });
+        // a head's maximum: over the lanes (and places) with sums of this head
 #pragma unroll
         for (int h = 0; h < HB; ++h) {
+            float x = -INFINITY;
 #pragma unroll
-            for (int o = 16; o >= LPK; o >>= 1) m[h] = fmaxf(m[h], __shfl_xor_sync(0xffffffffu, m[h], o));
-            if (lane == 0) warp_max[h] = m[h];
+            for (int l = 0; l < Sums::LEFT; ++l) x = (sum0 + l) % HB == h ? fmaxf(x, m[l]) : x;
+#pragma unroll
+            for (int o = 16; o > 0; o >>= 1) x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, o));
+            if (lane == 0) warp_max[h] = x;
         }
     }
 
     template <typename Max, typename Get>
-    __device__ __forceinline__ void values(const PagedArgs& a, int nh, const T* V, const int64_t* off, int count, PagedExp exp, float* warp_sum,
-                                           float* warp_out, Max first, Get get)
+    static __device__ __forceinline__ void values(const PagedArgs& a, int nh, const T* V, const int64_t* off, int count, PagedExp exp, unsigned char* ring,
+                                                  float* warp_sum, Max maxima, Get get)
     {
-        const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, part = lane & (LPK - 1), sub = lane / LPK;
-        float acc[HB][VPL][N], sum[HB], m[HB];
-        const float* maxima = first();
+        const int lane = threadIdx.x & 31, part = lane & (LPK - 1), sub = lane / LPK;
+        const uint32_t ring_at = nm_smem_u32(ring);
+        constexpr int TH = U * HB;   // a token's exponentials are shared by its lanes: lane `part` computes number part, part + LPK, ...
+        constexpr int MINE = (TH + LPK - 1) / LPK;
+        float acc[HB][VPL][N], sum[MINE], m[MINE];
+        paged_pipeline<STAGES, TILE>(
+            count, [&](int i0, int stage) { fetch(a, V, off, count, ring_at, i0, stage); },
+            [&] {
+                const float* x = maxima();
 #pragma unroll
-        for (int h = 0; h < HB; ++h) {
-            sum[h] = 0.f;
-            m[h] = maxima[h];
-#pragma unroll
-            for (int v = 0; v < VPL; ++v)
-#pragma unroll
-                for (int e = 0; e < N; ++e) acc[h][v][e] = 0.f;
-        }
-        for (int i = warp * TILE + sub; i < count; i += PAGED_WARPS * TILE) {
-            const int64_t at = off[i];
-            Vec16<T> x[VPL];
-#pragma unroll
-            for (int v = 0; v < VPL; ++v) {
-                const int c = (v * LPK + part) * N;
-                x[v].raw = at >= 0 && c < a.d.d ? __ldg(reinterpret_cast<const uint4*>(V + at + c)) : make_uint4(0, 0, 0, 0);
-            }
-            float e[HB];
-#pragma unroll
-            for (int h = 0; h < HB; ++h) {
-                float s = 0.f;
-                if (h < nh) {
-                    const float2 two = get(h, i & ~1);
-                    s = exp((i & 1 ? two.y : two.x) - m[h]);
+                for (int l = 0; l < MINE; ++l) {
+                    m[l] = x[(l * LPK + part) % HB];
+                    sum[l] = 0.f;
                 }
-                e[h] = s;
-                sum[h] += s;
-            }
-#pragma unroll
-            for (int v = 0; v < VPL; ++v) {
-                float f[N];
-                x[v].get(f);
 #pragma unroll
                 for (int h = 0; h < HB; ++h)
 #pragma unroll
-                    for (int k = 0; k < N; ++k) acc[h][v][k] = __fmaf_rn(e[h], f[k], acc[h][v][k]);
-            }
-        }
-        __syncthreads();   // scores and offsets have been read: warp_out may lie over them
+                    for (int v = 0; v < VPL; ++v)
+#pragma unroll
+                        for (int e = 0; e < N; ++e) acc[h][v][e] = 0.f;
+            },
+            [&](int i0, int stage) {
+                const uint4* tile = reinterpret_cast<const uint4*>(ring + stage * STAGE) + lane;
+                float mine[MINE];
+#pragma unroll
+                for (int l = 0; l < MINE; ++l) {
+                    const int x = l * LPK + part, h = x % HB, i = i0 + x / HB * SUB + sub;
+                    mine[l] = x < TH && h < nh && i < count ? exp(get(h, i) - m[l]) : 0.f;
+                    sum[l] += mine[l];
+                }
+#pragma unroll
+                for (int k = 0; k < U; ++k) {
+                    float e[HB];
+#pragma unroll
+                    for (int h = 0; h < HB; ++h)
+                        e[h] = __shfl_sync(0xffffffffu, mine[(k * HB + h) / LPK], (lane & ~(LPK - 1)) | ((k * HB + h) % LPK));
+#pragma unroll
+                    for (int v = 0; v < VPL; ++v) {
+                        Vec16<T> x;
+                        x.raw = tile[(k * VPL + v) * 32];
+                        float f[N];
+                        x.get(f);
+#pragma unroll
+                        for (int h = 0; h < HB; ++h)
+#pragma unroll
+                            for (int c = 0; c < N; ++c) acc[h][v][c] = __fmaf_rn(e[h], f[c], acc[h][v][c]);
+                    }
+                }
+            });
+        __syncwarp();   // the ring has been read
+        float* out = reinterpret_cast<float*>(ring);
 #pragma unroll
         for (int h = 0; h < HB; ++h) {
+            float s = 0.f;
 #pragma unroll
-            for (int o = 16; o >= LPK; o >>= 1) {
-                sum[h] += __shfl_xor_sync(0xffffffffu, sum[h], o);
+            for (int l = 0; l < MINE; ++l) s += (l * LPK + part) % HB == h ? sum[l] : 0.f;
 #pragma unroll
-                for (int v = 0; v < VPL; ++v)
+            for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+            if (lane == 0) warp_sum[h] = s;
 #pragma unroll
-                    for (int k = 0; k < N; ++k) acc[h][v][k] += __shfl_xor_sync(0xffffffffu, acc[h][v][k], o);
+            for (int v = 0; v < VPL; ++v) {
+#pragma unroll
+                for (int c = 0; c < N; ++c) {
+#pragma unroll
+                    for (int o = 16; o >= LPK; o >>= 1) acc[h][v][c] += __shfl_xor_sync(0xffffffffu, acc[h][v][c], o);
+                    if (sub == 0) out[h * D + (v * LPK + part) * N + c] = acc[h][v][c];
+                }
             }
-            if (sub == 0) {
-#pragma unroll
-                for (int v = 0; v < VPL; ++v)
-#pragma unroll
-                    for (int k = 0; k < N; ++k) warp_out[h * D + (v * LPK + part) * N + k] = acc[h][v][k];
-            }
-            if (lane == 0) warp_sum[h] = sum[h];
         }
     }
 };
@@ -411,17 +531,12 @@ template <class Core> __device__ __forceinline__ PagedUnit paged_unit(const Page
     u.nh = min(Core::HEADS, a.group - hb * Core::HEADS);
     return u;
 }
-template <class Core> __host__ __device__ constexpr size_t paged_out_bytes() { return (size_t)PAGED_WARPS * Core::HEADS * Core::D * 4; }
 // scores of a block: rows of this many floats (8 beyond a multiple of 32: eight heads' pairs lie in different banks)
 __host__ __device__ constexpr int paged_pitch(int span) { return (span + 31) / 32 * 32 + 8; }
-template <class Core> size_t paged_fused_bytes(int span)
+template <class Core> constexpr size_t paged_split_bytes(int span) { return (size_t)PAGED_WARPS * Core::RING + (size_t)span * 8; }
+template <class Core> constexpr size_t paged_fused_bytes(int span)
 {
-    const size_t work = (size_t)span * 8 + (size_t)Core::HEADS * paged_pitch(span) * 4;
-    return work > paged_out_bytes<Core>() ? work : paged_out_bytes<Core>();
-}
-template <class Core> size_t paged_values_bytes(int span)
-{
-    return (size_t)span * 8 > paged_out_bytes<Core>() ? (size_t)span * 8 : paged_out_bytes<Core>();
+    return paged_split_bytes<Core>(span) + (size_t)Core::HEADS * paged_pitch(span) * 4;
 }
 
 #define NM_PAGED_EXP_TABLE()                                                                             \
@@ -447,17 +562,16 @@ __global__ void __launch_bounds__(PAGED_THREADS, 2) paged_fused_kernel(const Pag
     const int len = paged_length(a, u.b);
     if (len < 0) return;   // the whole cluster
     const int per = ((len + (int)ctas - 1) / (int)ctas + 15) / 16 * 16, first = min(len, rank * per), count = min(len - first, per);
-    int64_t* off = reinterpret_cast<int64_t*>(paged_smem);
-    float* sc = reinterpret_cast<float*>(paged_smem + (size_t)a.span * 8);
     const int pitch = paged_pitch(a.span), warp = threadIdx.x >> 5;
+    unsigned char* ring = paged_smem + warp * Core::RING;
+    int64_t* off = reinterpret_cast<int64_t*>(paged_smem + PAGED_WARPS * Core::RING);
+    float* sc = reinterpret_cast<float*>(off + a.span);
     paged_offsets(a, u.b, first, count, off);
     __syncthreads();
     Core::scores(a, (const T*)a.d.Q + (int64_t)u.b * a.d.ld_q + (int64_t)u.h0 * a.d.d, u.nh, (const T*)a.d.k_cache + (int64_t)u.kv * a.d.stride_head,
-                 off, count, s_max[warp], [&](int h, int i, float s) { sc[h * pitch + i] = s; });
-    Core core;
-    float* out = reinterpret_cast<float*>(paged_smem);
-    core.values(
-        a, u.nh, (const T*)a.d.v_cache + (int64_t)u.kv * a.d.stride_head, off, count, exp, s_sum[warp], out + warp * (Core::HEADS * Core::D),
+                 off, count, ring, s_max[warp], [&](int h, int i, float s) { sc[h * pitch + i] = s; });
+    Core::values(
+        a, u.nh, (const T*)a.d.v_cache + (int64_t)u.kv * a.d.stride_head, off, count, exp, ring, s_sum[warp],
         [&] {   // the row's maxima
             __syncthreads();
             if (threadIdx.x < Core::HEADS) {
@@ -482,12 +596,13 @@ __global__ void __launch_bounds__(PAGED_THREADS, 2) paged_fused_kernel(const Pag
             __syncthreads();
             return (const float*)s_row_max;
         },
-        [&](int h, int i) { return *reinterpret_cast<const float2*>(sc + h * pitch + i); });
+        [&](int h, int i) { return Core::read(sc + h * pitch + i); });
     __syncthreads();
     // the block's sums in warp 0's place
+    float* out = reinterpret_cast<float*>(paged_smem);
     for (int x = threadIdx.x; x < u.nh * Core::D; x += PAGED_THREADS) {
         float o = out[x];
-        for (int w = 1; w < PAGED_WARPS; ++w) o += out[w * (Core::HEADS * Core::D) + x];
+        for (int w = 1; w < PAGED_WARPS; ++w) o += out[w * (Core::RING / 4) + x];
         out[x] = o;
     }
     if (threadIdx.x < Core::HEADS) {
@@ -526,12 +641,13 @@ __global__ void __launch_bounds__(PAGED_THREADS, 2) paged_scores_kernel(const Pa
     const int len = paged_length(a, u.b);
     if (first >= len) return;
     const int count = min(len - first, a.span);
-    int64_t* off = reinterpret_cast<int64_t*>(paged_smem);
+    unsigned char* ring = paged_smem + (threadIdx.x >> 5) * Core::RING;
+    int64_t* off = reinterpret_cast<int64_t*>(paged_smem + PAGED_WARPS * Core::RING);
     paged_offsets(a, u.b, first, count, off);
     __syncthreads();
     float* sc = a.scores + ((int64_t)u.b * a.d.heads + u.h0) * a.row + first;
     Core::scores(a, (const T*)a.d.Q + (int64_t)u.b * a.d.ld_q + (int64_t)u.h0 * a.d.d, u.nh, (const T*)a.d.k_cache + (int64_t)u.kv * a.d.stride_head,
-                 off, count, s_max[threadIdx.x >> 5], [&](int h, int i, float s) {
+                 off, count, ring, s_max[threadIdx.x >> 5], [&](int h, int i, float s) {
                      if (h < u.nh) sc[h * a.row + i] = s;
                  });
     __syncthreads();
@@ -556,7 +672,8 @@ __global__ void __launch_bounds__(PAGED_THREADS, 2) paged_values_kernel(const Pa
     const int len = paged_length(a, u.b);
     if (first >= len) return;
     const int count = min(len - first, a.span), used = (len + a.span - 1) / a.span;
-    int64_t* off = reinterpret_cast<int64_t*>(paged_smem);
+    unsigned char* ring = paged_smem + warp * Core::RING;
+    int64_t* off = reinterpret_cast<int64_t*>(paged_smem + PAGED_WARPS * Core::RING);
     paged_offsets(a, u.b, first, count, off);
     const int64_t head0 = (int64_t)u.b * a.d.heads + u.h0;
     for (int h = warp; h < Core::HEADS; h += PAGED_WARPS) {
@@ -569,17 +686,16 @@ __global__ void __launch_bounds__(PAGED_THREADS, 2) paged_values_kernel(const Pa
     }
     __syncthreads();
     const float* sc = a.scores + head0 * a.row + first;
-    Core core;
-    float* out = reinterpret_cast<float*>(paged_smem);
-    core.values(a, u.nh, (const T*)a.d.v_cache + (int64_t)u.kv * a.d.stride_head, off, count, exp, s_sum[warp], out + warp * (Core::HEADS * Core::D),
-                [&] { return (const float*)s_m; }, [&](int h, int i) { return *reinterpret_cast<const float2*>(sc + h * a.row + i); });
+    Core::values(a, u.nh, (const T*)a.d.v_cache + (int64_t)u.kv * a.d.stride_head, off, count, exp, ring, s_sum[warp], [&] { return (const float*)s_m; },
+                 [&](int h, int i) { return Core::read(sc + h * a.row + i); });
     __syncthreads();
     for (int x = threadIdx.x; x < u.nh * Core::D; x += PAGED_THREADS) {
         const int h = x / Core::D, c = x - h * Core::D;
         if (c >= a.d.d) continue;
+        const float* out = reinterpret_cast<const float*>(paged_smem);
         float o = out[x], s = s_sum[0][h];
         for (int w = 1; w < PAGED_WARPS; ++w) {
-            o += out[w * (Core::HEADS * Core::D) + x];
+            o += out[w * (Core::RING / 4) + x];
             s += s_sum[w][h];
         }
         const int64_t row = (head0 + h) * a.spans + span;
@@ -588,23 +704,41 @@ __global__ void __launch_bounds__(PAGED_THREADS, 2) paged_values_kernel(const Pa
     }
 }
 
-// A block per request and head.
+// A block per request and head: four warps take every fourth span, a lane four channels of a span.
+constexpr int JOIN_WARPS = 4;
 template <typename T>
-__global__ void __launch_bounds__(128) paged_join_kernel(const PagedArgs a)
+__global__ void __launch_bounds__(JOIN_WARPS * 32) paged_join_kernel(const PagedArgs a)
 {
+    __shared__ float s_out[JOIN_WARPS][256], s_sum[JOIN_WARPS];
     const int64_t bh = blockIdx.x;
-    const int b = (int)(bh / a.d.heads), h = (int)(bh - (int64_t)b * a.d.heads);
+    const int b = (int)(bh / a.d.heads), h = (int)(bh - (int64_t)b * a.d.heads), lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     nm_grid_launch_dependents();
     nm_grid_dependency_wait();
     const int len = paged_length(a, b);
     if (len < 0) return;
     const int used = (len + a.span - 1) / a.span;
     float s = 0.f;
-    for (int i = 0; i < used; ++i) s += a.sums[bh * a.spans + i];
+    for (int i = warp * 32 + lane; i < used; i += JOIN_WARPS * 32) s += a.sums[bh * a.spans + i];
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+    if (lane == 0) s_sum[warp] = s;
+    for (int c = lane * 4; c < a.d.d; c += 128) {
+        float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 4
+        for (int i = warp; i < used; i += JOIN_WARPS) {
+            const float4 v = *reinterpret_cast<const float4*>(a.outs + (bh * a.spans + i) * a.d.d + c);
+            o.x += v.x;
+            o.y += v.y;
+            o.z += v.z;
+            o.w += v.w;
+        }
+        *reinterpret_cast<float4*>(&s_out[warp][c]) = o;
+    }
+    __syncthreads();
+    s = s_sum[0] + s_sum[1] + s_sum[2] + s_sum[3];
     const float r = paged_table(a.recip_tab, s);
-    for (int c = threadIdx.x; c < a.d.d; c += 128) {
-        float o = 0.f;
-        for (int i = 0; i < used; ++i) o += a.outs[(bh * a.spans + i) * a.d.d + c];
+    for (int c = threadIdx.x; c < a.d.d; c += JOIN_WARPS * 32) {
+        const float o = s_out[0][c] + s_out[1][c] + s_out[2][c] + s_out[3][c];
         ((T*)a.d.out)[(int64_t)b * a.d.ld_out + (int64_t)h * a.d.d + c] = NmType<T>::from_f(used ? o * r : 0.f);
     }
 }
@@ -620,6 +754,8 @@ int paged_heads(const nm_attn_paged_desc* d, bool mma)
     if (mma) return group > 8 && d->d <= 128 ? 16 : 8;
     return group >= 8 ? 8 : group >= 4 ? 4 : group >= 2 ? 2 : 1;
 }
+// Tokens of a block of the fused form: offsets and scores take what rings of 64 KB leave of half an SM's shared memory.
+int paged_cap(int heads) { return (44 * 1024 - heads * 4 * 40) / (8 + heads * 4) / 16 * 16; }
 bool paged_mma_supported(const nm_attn_paged_desc* d) { return d->dtype != NM_F32 && (d->d == 64 || d->d == 96 || d->d == 128 || d->d == 256); }
 
 struct PagedLayout {
@@ -639,7 +775,7 @@ PagedLayout layout_of(const nm_attn_paged_desc* d)
     l.scores = l.maxima = l.sums = l.outs = l.total = 0;
     l.row = 0;
     l.spans = 1;
-    const int cap = l.heads == 16 ? 1024 : 2048;   // two blocks an SM
+    const int cap = paged_cap(l.heads);
     l.fused = d->max_len <= 8 * cap;
     if (l.fused) {
         int ctas = 1;
@@ -680,11 +816,11 @@ nm_status launch(nm_ctx* ctx, const PagedArgs& a, const PagedLayout& l, cudaStre
     using T = typename Core::Elem;
     const double bytes = (double)a.d.B * a.d.max_len * a.d.kv_heads * a.d.d * sizeof(T);
     if (l.fused) return paged_launch(ctx, paged_fused_kernel<Core>, a, l.units * l.ctas, PAGED_THREADS, paged_fused_bytes<Core>(l.span), l.ctas, 2 * bytes, st);
-    nm_status s = paged_launch(ctx, paged_scores_kernel<Core>, a, l.units * l.spans, PAGED_THREADS, (size_t)l.span * 8, 1, bytes, st);
+    nm_status s = paged_launch(ctx, paged_scores_kernel<Core>, a, l.units * l.spans, PAGED_THREADS, paged_split_bytes<Core>(l.span), 1, bytes, st);
     if (s != NM_OK) return s;
-    s = paged_launch(ctx, paged_values_kernel<Core>, a, l.units * l.spans, PAGED_THREADS, paged_values_bytes<Core>(l.span), 1, bytes, st);
+    s = paged_launch(ctx, paged_values_kernel<Core>, a, l.units * l.spans, PAGED_THREADS, paged_split_bytes<Core>(l.span), 1, bytes, st);
     if (s != NM_OK) return s;
-    return paged_launch(ctx, paged_join_kernel<T>, a, (int64_t)a.d.B * a.d.heads, 128, 0, 1, 0.0, st);
+    return paged_launch(ctx, paged_join_kernel<T>, a, (int64_t)a.d.B * a.d.heads, JOIN_WARPS * 32, 0, 1, 0.0, st);
 }
 
 template <typename T>
