@@ -2,31 +2,33 @@
 //
 // A PWL exponential is not multiplicative, so e_j = PWL_exp(s_j - m) needs the maximum m of the whole row before the first value is
 // weighted: a running maximum that rescales earlier sums would compute another function.  Keys and values are still read once
-// each, because the scores are kept (4 bytes per token and query head, against 2 d elements of K and V per token and key head):
-//   fused   a cluster of blocks per request and key head, scores in shared memory, maxima and sums exchanged within the cluster
-//   split   rows longer than a cluster holds: one launch for the scores (to the workspace), one for the values, one that joins
-// A unit of work is a request, a key head and up to HEADS of its query heads; its tokens are split over blocks, a block's over its
-// warps in tiles.  Two cores do a tile:
-//   PagedMma   16-bit types, d a multiple of 32: m16n8k16 products, fragments loaded from the cache straight into registers
+// each, because the scores are kept (4 bytes per token and query head, against 2 d elements of K and V per token and key head).
+// A unit of work is a request, a key head and up to HEADS of its query heads.
+//   fused   one launch: a cluster of blocks per unit, scores in shared memory, maxima and sums exchanged within the cluster
+//   split   two launches, scores in the workspace: all units' tokens lie one after another and every block takes an equal share, so
+//           that requests of any lengths keep all SMs busy to the end; a unit that several blocks have is joined by the last of them
+// A block's tokens are split over its warps in tiles.  Two cores do a tile:
+//   PagedMma   16-bit types, d a multiple of 32: m16n8k16 products
 //   PagedFma   fp32 and other d: FMAs, a few lanes per token
 // Partial sums are fp32 and are added in the order of warps and blocks: results do not depend on timing.
 #include "nm_common.cuh"
 
 namespace {
 
-#ifndef RINGB
-#define RINGB 8192
-#endif
-constexpr int PAGED_WARPS = 8, PAGED_THREADS = PAGED_WARPS * 32, PAGED_RING = RINGB;   // bytes of a warp's ring
+constexpr int PAGED_WARPS = 8, PAGED_THREADS = PAGED_WARPS * 32, PAGED_RING = 8192;   // bytes of a warp's ring
 
 struct PagedArgs {
     nm_attn_paged_desc d;
     const NmTable *exp_tab, *recip_tab;
     int* status;
     int group, blocks_per_head;   // query heads of a key head; units that they make
-    int span, spans;              // split: tokens of a block, blocks of a row; fused: tokens that a block's shared memory holds
+    int64_t page_bytes, token_bytes;      // distances of pages and tokens in the caches
+    uint32_t div_mul, div_shift;          // j / page_size = umulhi(j, div_mul) >> div_shift for every token number j (page_size > 1)
+    int span;                     // fused: tokens that a block's shared memory holds; split: tokens that a block has at least
     int64_t row;                  // split: scores of one head in the workspace
-    float *scores, *maxima, *sums, *outs;   // split: [B][heads][row], [B][heads][spans], [B][heads][spans], [B][heads][spans][d]
+    float *scores, *maxima;       // split: [B][heads][row]; [B][heads], of units that one block has
+    float *part_max, *parts;      // split, two places per block: [HEADS]; [HEADS][d] and [HEADS], unit sums not yet joined
+    int* tickets;                 // split: per block, how many blocks have finished the unit that begins in it and goes on
 };
 
 __device__ __forceinline__ float paged_table(const NmTable* t, float x)
@@ -35,14 +37,18 @@ __device__ __forceinline__ float paged_table(const NmTable* t, float x)
     return __fmaf_rn(kb.x, x, kb.y);
 }
 
-// The exponential's table in shared memory.
+// The exponential's table in shared memory.  floor(u) is taken by adding 1.5 * 2^23 with rounding down, which leaves it in the low bits
+// (0 <= u < 2^22), and the entry's address is formed from those.
 struct PagedExp {
-    const float2* kb;
+    uint32_t at;   // shared address of the table, less what the bits of 1.5 * 2^23 add to it
     float inv_h, off, nm1;
     __device__ __forceinline__ float operator()(float x) const
     {
-        const float2 v = kb[nm_pwl_index(x, inv_h, off, nm1)];
-        return __fmaf_rn(v.x, x, v.y);
+        const float u = fminf(fmaxf(__fmaf_rn(x, inv_h, off), 0.0f), nm1);
+        const uint32_t entry = (__float_as_uint(__fadd_rd(u, 12582912.0f)) << 3) + at;
+        float k, b;
+        asm("ld.shared.v2.f32 {%0, %1}, [%2];" : "=f"(k), "=f"(b) : "r"(entry));   // the table is only read
+        return __fmaf_rn(k, x, b);
     }
 };
 
@@ -57,50 +63,86 @@ __device__ __forceinline__ int paged_length(const PagedArgs& a, int b)
     return n;
 }
 
-// Element offsets of the block's tokens in K and V (without the head); -1 for a page that the cache does not have (recorded).
-__device__ __forceinline__ void paged_offsets(const PagedArgs& a, int b, int first, int count, int64_t* off)
-{
-    const int32_t* table = a.d.block_tables + (int64_t)b * a.d.ld_tables;
-    for (int i = threadIdx.x; i < count; i += PAGED_THREADS) {
-        const int j = first + i, entry = j / a.d.page_size, page = table[entry];
-        if (page < 0 || page >= a.d.num_pages) {
-            atomicExch(a.status, (int)NM_ERR_INVALID_ARG);
-            off[i] = -1;
-        } else {
-            off[i] = (int64_t)page * a.d.stride_page + (int64_t)(j - entry * a.d.page_size) * a.d.stride_token;
-        }
-    }
-}
+// The tokens of one unit that a block works on.
+struct PagedTokens {
+    const int32_t* table;   // the request's
+    int first, count;
+};
 
-// Asynchronous copies: a warp copies what it will read itself, so its tiles need no barrier of the block.  Invalid tokens are filled
-// with zeros.
-__device__ __forceinline__ void paged_copy(uint32_t dst, const void* src, bool valid)
+// Where a warp's next tiles are: byte offsets from the key head's first token in K and V.  Tokens of a page that the cache does not have
+// (recorded) and those that fill up the last tile are PAGED_NONE, read as zeros.  The lanes look up a round of 32 tokens at a time
+// (32 / TILE tiles of the warp); the next round's pages are on their way meanwhile.
+constexpr int64_t PAGED_NONE = -1;
+template <int TILE> struct PagedCursor {
+    static constexpr int TILES = 32 / TILE, STEP = 32 * PAGED_WARPS;   // tokens of the block's warps in a round
+    const PagedArgs& a;
+    const PagedTokens& tok;
+    int64_t* buf;   // two rounds, the warp's own
+    int token, page, place;   // the lane's token of the next round; its page and place
+    uint32_t live;  // lanes of the current round with a token to read
+
+    __device__ __forceinline__ PagedCursor(const PagedArgs& args, const PagedTokens& t, int64_t* b) : a(args), tok(t), buf(b), live(0)
+    {
+        const int lane = threadIdx.x & 31;
+        token = (threadIdx.x >> 5) * TILE + lane / TILE * (PAGED_WARPS * TILE) + lane % TILE;
+        look();
+    }
+    __device__ __forceinline__ void look()
+    {
+        const int j = tok.first + token, entry = a.d.page_size == 1 ? j : (int)(__umulhi((uint32_t)j, a.div_mul) >> a.div_shift);
+        place = j - entry * a.d.page_size;
+        page = token < tok.count ? tok.table[entry] : -1;
+    }
+    // offsets of the warp's tile number n (one after another from 0); *whole: all of its tokens are there
+    __device__ __forceinline__ const int64_t* tile(int n, bool* whole)
+    {
+        int64_t* at = buf + (n / TILES & 1) * 32;
+        if (n % TILES == 0) {
+            const bool good = (uint32_t)page < (uint32_t)a.d.num_pages;
+            if (!good && token < tok.count) atomicExch(a.status, (int)NM_ERR_INVALID_ARG);
+            at[threadIdx.x & 31] = good ? (int64_t)page * a.page_bytes + (int64_t)place * a.token_bytes : PAGED_NONE;
+            live = __ballot_sync(0xffffffffu, good);   // (and the lanes' offsets are there)
+            __syncwarp();
+            token += STEP;
+            look();
+        }
+        constexpr uint32_t ALL = TILE == 32 ? 0xffffffffu : (1u << (TILE & 31)) - 1;
+        *whole = (live >> (n % TILES * TILE) & ALL) == ALL;
+        return at + n % TILES * TILE;
+    }
+};
+
+// Asynchronous copies of 16 bytes of a token: a warp copies what it will read itself, so its tiles need no barrier of the block.
+__device__ __forceinline__ void paged_copy(uint32_t dst, const uint8_t* src) { asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory"); }
+__device__ __forceinline__ void paged_copy_or_zero(uint32_t dst, const uint8_t* base, int64_t off)
 {
-    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(valid ? 16 : 0) : "memory");
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(off < 0 ? base : base + off), "r"(off < 0 ? 0 : 16) : "memory");
 }
 __device__ __forceinline__ void paged_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int N> __device__ __forceinline__ void paged_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
 
-// Runs a warp's tiles through its ring: fetch(i0, stage) starts the copies of the tile at token i0, use(i0, stage) consumes it.  `ready` is
-// called once the first tiles are on their way.
-template <int STAGES, int TILE, typename Fetch, typename Ready, typename Use>
-__device__ __forceinline__ void paged_pipeline(int count, Fetch fetch, Ready ready, Use use)
+// Runs a warp's tiles through its ring: fetch(n, stage) starts the copies of its tile number n, take(stage) brings a tile from the ring
+// to registers, after which the stage is filled again, use(i0) works on the registers.  So all stages are on their way while a tile is
+// worked on.  `ready` is called once the first tiles are on their way.
+template <int STAGES, int TILE, typename Fetch, typename Ready, typename Take, typename Use>
+__device__ __forceinline__ void paged_pipeline(int count, Fetch fetch, Ready ready, Take take, Use use)
 {
     constexpr int STEP = PAGED_WARPS * TILE;
-    int i0 = (threadIdx.x >> 5) * TILE, next = i0, stage = 0;
+    int i0 = (threadIdx.x >> 5) * TILE, next = i0, n = 0, stage = 0;
 #pragma unroll
-    for (int s = 0; s < STAGES - 1; ++s, next += STEP) {
-        if (next < count) fetch(next, s);
+    for (int s = 0; s < STAGES; ++s, next += STEP) {
+        if (next < count) fetch(n++, s);
         paged_commit();
     }
     ready();
     for (; i0 < count; i0 += STEP, next += STEP) {
-        if (next < count) fetch(next, stage == 0 ? STAGES - 1 : stage - 1);   // the stage that the tile before has left
-        paged_commit();
         paged_wait<STAGES - 1>();
         __syncwarp();   // the lanes' copies are there
-        use(i0, stage);
+        take(stage);
         __syncwarp();   // and have been read
+        if (next < count) fetch(n++, stage);
+        paged_commit();
+        use(i0);
         stage = stage == STAGES - 1 ? 0 : stage + 1;
     }
     paged_wait<0>();
@@ -149,42 +191,57 @@ __device__ __forceinline__ void paged_ldmatrix_trans(uint32_t* r, uint32_t at)
                  : "memory");
 }
 
-// Tiles of 16 tokens, NT tiles of 8 query heads: S^T = K Q^T and O^T = V^T P^T, tokens or channels as rows, so that eight heads fill
-// a product.  Rows are copied whole (fragments loaded from the cache directly would take 64 bytes of a row at a time: 2.9 to 4.9 TB/s
-// where whole rows reach ...) and lie in the ring with their 16-byte pieces permuted, piece c of row r at c ^ (r & 7)
-// (rows of 96 channels one piece apart instead): neither the copies nor the matrix reads collide.
-// Probabilities are two 16-bit terms.
+// Tiles of MT * 16 tokens, NT tiles of 8 query heads: S^T = K Q^T and O^T = V^T P^T, tokens or channels as rows, so that eight heads fill
+// a product.  Rows are copied whole and lie in the ring with their 16-byte pieces permuted, piece c of row r at c ^ (r & 7) (rows of
+// 96 channels one piece apart instead): neither the copies nor the matrix reads collide.  Probabilities are two 16-bit terms.
 template <typename T, int D_, int NT> struct PagedMma {
     using Elem = T;
-    static constexpr int D = D_, HEADS = NT * 8, TILE = 16, LANES = D / 8;   // lanes of a row
+    static constexpr int D = D_, HEADS = NT * 8, MT = D <= 64 ? 2 : 1, TILE = 16 * MT, LANES = D / 8;   // lanes of a row
     static constexpr bool POW2 = (LANES & (LANES - 1)) == 0;
-    static constexpr int PITCH = D * 2 + (POW2 ? 0 : 16), STAGE = TILE * PITCH, STAGES = PAGED_RING / STAGE < 2 ? 2 : PAGED_RING / STAGE, RING = STAGES * STAGE;   // bytes of a warp
+    static constexpr int PITCH = D * 2 + (POW2 ? 0 : 16), STAGE = TILE * PITCH, STAGES = PAGED_RING / STAGE < 2 ? 2 : PAGED_RING / STAGE;
+    static constexpr int RING = STAGES * STAGE;   // bytes of a warp
     static_assert(D % 32 == 0 && HEADS * D * 4 <= RING, "whole 32-channel pieces; a warp's sums fit its ring");
     static __device__ __forceinline__ float2 read(const float* s) { return *reinterpret_cast<const float2*>(s); }   // two tokens' scores
 
     static __device__ __forceinline__ uint32_t piece(int row, int c) { return row * PITCH + ((POW2 ? c ^ (row & 7) : c) << 4); }
-    static __device__ __forceinline__ void fetch(const T* base, const int64_t* off, int count, uint32_t ring_at, int i0, int stage)
+    static __device__ __forceinline__ void fetch(const T* base, PagedCursor<TILE>& cursor, uint32_t ring_at, int n, int stage)
     {
         const int lane = threadIdx.x & 31;
+        bool whole;
+        const int64_t* off = cursor.tile(n, &whole);
+        const uint32_t to = ring_at + stage * STAGE;
+        if constexpr (POW2) {   // the lane has one place in every row that it copies
+            const uint8_t* from = (const uint8_t*)base + lane % LANES * 16;
+            constexpr int STEP = 32 / LANES;   // rows of a copy
+            if (whole) {
 #pragma unroll
-        for (int x = 0; x < TILE * LANES / 32; ++x) {
-            const int at = x * 32 + lane, row = at / LANES, c = at % LANES, i = i0 + row;
-            const int64_t o = i < count ? off[i] : -1;
-            paged_copy(ring_at + stage * STAGE + piece(row, c), o >= 0 ? base + o + c * 8 : base, o >= 0);
+                for (int x = 0; x < TILE / STEP; ++x) paged_copy(to + piece(x * STEP + lane / LANES, lane % LANES), from + off[x * STEP + lane / LANES]);
+            } else {
+#pragma unroll
+                for (int x = 0; x < TILE / STEP; ++x)
+                    paged_copy_or_zero(to + piece(x * STEP + lane / LANES, lane % LANES), from, off[x * STEP + lane / LANES]);
+            }
+        } else {
+#pragma unroll
+            for (int x = 0; x < TILE * LANES / 32; ++x) {
+                const int at = x * 32 + lane, row = at / LANES, c = at % LANES;
+                paged_copy_or_zero(to + piece(row, c), (const uint8_t*)base + c * 16, off[row]);
+            }
         }
     }
 
     // put(h, i, s) takes the score of head h and token i; the heads' maxima over the warp's tokens go to warp_max
     template <typename Put>
-    static __device__ __forceinline__ void scores(const PagedArgs& a, const T* Q, int nh, const T* K, const int64_t* off, int count, unsigned char* ring,
-                                                  float* warp_max, Put put)
+    static __device__ __forceinline__ void scores(const PagedArgs& a, const T* Q, int nh, const T* K, const PagedTokens& tok, unsigned char* ring,
+                                                  int64_t* offsets, float* warp_max, Put put)
     {
-        const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
+        const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3, count = tok.count;
         const uint32_t ring_at = nm_smem_u32(ring);
-        uint32_t q[NT][D / 16][2];
+        PagedCursor<TILE> cursor(a, tok, offsets);
+        uint32_t q[NT][D / 16][2], k[MT][D / 16][4];
         float m[NT][2];
         paged_pipeline<STAGES, TILE>(
-            count, [&](int i0, int stage) { fetch(K, off, count, ring_at, i0, stage); },
+            count, [&](int n, int stage) { fetch(K, cursor, ring_at, n, stage); },
             [&] {
 #pragma unroll
                 for (int n = 0; n < NT; ++n) {
@@ -196,29 +253,41 @@ template <typename T, int D_, int NT> struct PagedMma {
                             q[n][c][r] = n * 8 + g < nh ? *reinterpret_cast<const uint32_t*>(Q + (n * 8 + g) * D + c * 16 + r * 8 + t * 2) : 0;
                 }
             },
-            [&](int i0, int stage) {
-                float s[NT][4];
+            [&](int stage) {
 #pragma unroll
-                for (int n = 0; n < NT; ++n) s[n][0] = s[n][1] = s[n][2] = s[n][3] = 0.f;
-                const uint32_t tile = ring_at + stage * STAGE;
+                for (int x = 0; x < MT; ++x)
 #pragma unroll
-                for (int c = 0; c < D / 16; ++c) {
-                    uint32_t k[4];
-                    paged_ldmatrix(k, tile + piece(lane & 15, 2 * c + (lane >> 4)));
+                    for (int c = 0; c < D / 16; ++c) paged_ldmatrix(k[x][c], ring_at + stage * STAGE + piece(x * 16 + (lane & 15), 2 * c + (lane >> 4)));
+            },
+            [&](int i0) {
+                float s[MT][NT][4], s2[MT][NT][4];   // two chains: a product waits for the one before it
 #pragma unroll
-                    for (int n = 0; n < NT; ++n) paged_mma(s[n], k[0], k[1], k[2], k[3], q[n][c][0], q[n][c][1], T());
-                }
+                for (int x = 0; x < MT; ++x)
 #pragma unroll
-                for (int n = 0; n < NT; ++n)
+                    for (int n = 0; n < NT; ++n)
 #pragma unroll
-                    for (int r = 0; r < 4; ++r) {
-                        const float v = s[n][r] * a.d.scale;
-                        const int j = i0 + g + (r >> 1) * 8;
-                        if (j < count) {
-                            m[n][r & 1] = fmaxf(m[n][r & 1], v);
-                            put(n * 8 + 2 * t + (r & 1), j, v);
+                        for (int r = 0; r < 4; ++r) s[x][n][r] = s2[x][n][r] = 0.f;
+#pragma unroll
+                for (int c = 0; c < D / 16; ++c)
+#pragma unroll
+                    for (int x = 0; x < MT; ++x)
+#pragma unroll
+                        for (int n = 0; n < NT; ++n)
+                            paged_mma(c & 1 ? s2[x][n] : s[x][n], k[x][c][0], k[x][c][1], k[x][c][2], k[x][c][3], q[n][c][0], q[n][c][1], T());
+                const bool whole = i0 + TILE <= count;
+#pragma unroll
+                for (int x = 0; x < MT; ++x)
+#pragma unroll
+                    for (int n = 0; n < NT; ++n)
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) {
+                            const float v = (s[x][n][r] + s2[x][n][r]) * a.d.scale;
+                            const int j = i0 + x * 16 + g + (r >> 1) * 8;
+                            if (whole || j < count) {
+                                m[n][r & 1] = fmaxf(m[n][r & 1], v);
+                                put(n * 8 + 2 * t + (r & 1), j, v);
+                            }
                         }
-                    }
             });
 #pragma unroll
         for (int n = 0; n < NT; ++n)
@@ -233,52 +302,80 @@ template <typename T, int D_, int NT> struct PagedMma {
     // get(h, i) reads the scores of head h and tokens i, i + 1; `maxima` is called once the first tiles are on their way.  The warp's
     // sums go to warp_sum and, as [head][channel], to the ring.
     template <typename Max, typename Get>
-    static __device__ __forceinline__ void values(const PagedArgs& a, int nh, const T* V, const int64_t* off, int count, PagedExp exp, unsigned char* ring,
-                                                  float* warp_sum, Max maxima, Get get)
+    static __device__ __forceinline__ void values(const PagedArgs& a, int nh, const T* V, const PagedTokens& tok, PagedExp exp, unsigned char* ring,
+                                                  int64_t* offsets, float* warp_sum, Max maxima, Get get)
     {
-        const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
+        const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3, count = tok.count;
         const uint32_t ring_at = nm_smem_u32(ring);
+        PagedCursor<TILE> cursor(a, tok, offsets);
+        uint32_t v[MT][D / 16][4];   // channels c * 16 + 0..7 and 8..15 of tokens 0..7, then of tokens 8..15
         float acc[NT][D / 16][4], sum[NT], m[NT];
-        paged_pipeline<STAGES, TILE>(
-            count, [&](int i0, int stage) { fetch(V, off, count, ring_at, i0, stage); },
-            [&] {
-                const float* x = maxima();
+        float2 next[MT][NT][2];   // scores of the next tile
+        // (heads behind the last one read its scores: their sums are dropped)
+        auto look = [&](int i0) {
 #pragma unroll
-                for (int n = 0; n < NT; ++n) {
-                    m[n] = x[n * 8 + g];
-                    sum[n] = 0.f;
-#pragma unroll
-                    for (int c = 0; c < D / 16; ++c) acc[n][c][0] = acc[n][c][1] = acc[n][c][2] = acc[n][c][3] = 0.f;
-                }
-            },
-            [&](int i0, int stage) {
-                uint32_t hi[NT][2], lo[NT][2];
+            for (int x = 0; x < MT; ++x)
 #pragma unroll
                 for (int n = 0; n < NT; ++n)
 #pragma unroll
                     for (int r = 0; r < 2; ++r) {
-                        const int i = i0 + 2 * t + r * 8;
-                        float x = 0.f, y = 0.f;
-                        if (n * 8 + g < nh && i < count) {
-                            const float2 s = get(n * 8 + g, i);   // a row's storage has whole tiles
-                            x = exp(s.x - m[n]);
-                            y = i + 1 < count ? exp(s.y - m[n]) : 0.f;
-                        }
-                        sum[n] += x + y;
-                        hi[n][r] = paged_term(x, y, T());
-                        lo[n][r] = paged_term(x, y, T());
+                        const int i = i0 + x * 16 + 2 * t + r * 8;   // a row's storage has whole 32s
+                        if (i < count) next[x][n][r] = get(min(n * 8 + g, nh - 1), i);
                     }
-                const uint32_t tile = ring_at + stage * STAGE;
+        };
+        paged_pipeline<STAGES, TILE>(
+            count, [&](int n, int stage) { fetch(V, cursor, ring_at, n, stage); },
+            [&] {
+                const float* x = maxima();
 #pragma unroll
-                for (int c = 0; c < D / 16; ++c) {
-                    uint32_t v[4];   // channels c * 16 + 0..7 and 8..15 of tokens 0..7, then of tokens 8..15
-                    paged_ldmatrix_trans(v, tile + piece((lane & 7) + (lane >> 4) * 8, 2 * c + ((lane >> 3) & 1)));
+                for (int n = 0; n < NT; ++n) {
+                    m[n] = x[min(n * 8 + g, nh - 1)];
+                    sum[n] = 0.f;
+#pragma unroll
+                    for (int c = 0; c < D / 16; ++c) acc[n][c][0] = acc[n][c][1] = acc[n][c][2] = acc[n][c][3] = 0.f;
+                }
+#pragma unroll
+                for (int y = 0; y < MT * NT * 2; ++y) next[y / (NT * 2)][y / 2 % NT][y & 1] = make_float2(0.f, 0.f);
+                look((threadIdx.x >> 5) * TILE);
+            },
+            [&](int stage) {
+#pragma unroll
+                for (int x = 0; x < MT; ++x)
+#pragma unroll
+                    for (int c = 0; c < D / 16; ++c)
+                        paged_ldmatrix_trans(v[x][c], ring_at + stage * STAGE + piece(x * 16 + (lane & 7) + (lane >> 4) * 8, 2 * c + ((lane >> 3) & 1)));
+            },
+            [&](int i0) {
+                const bool whole = i0 + TILE <= count;
+                uint32_t hi[MT][NT][2], lo[MT][NT][2];
+#pragma unroll
+                for (int x = 0; x < MT; ++x)
+#pragma unroll
+                    for (int n = 0; n < NT; ++n)
+#pragma unroll
+                        for (int r = 0; r < 2; ++r) {
+                            float p0 = exp(next[x][n][r].x - m[n]), p1 = exp(next[x][n][r].y - m[n]);
+                            if (!whole) {
+                                const int i = i0 + x * 16 + 2 * t + r * 8;
+                                p0 = i < count ? p0 : 0.f;
+                                p1 = i + 1 < count ? p1 : 0.f;
+                            }
+                            sum[n] += p0 + p1;
+                            hi[x][n][r] = paged_term(p0, p1, T());
+                            lo[x][n][r] = paged_term(p0, p1, T());
+                        }
+                look(i0 + PAGED_WARPS * TILE);
+#pragma unroll
+                for (int x = 0; x < MT; ++x)
 #pragma unroll
                     for (int n = 0; n < NT; ++n) {
-                        paged_mma(acc[n][c], v[0], v[1], v[2], v[3], hi[n][0], hi[n][1], T());
-                        paged_mma(acc[n][c], v[0], v[1], v[2], v[3], lo[n][0], lo[n][1], T());
+#pragma unroll
+                        for (int c = 0; c < D / 16; ++c)
+                            paged_mma(acc[n][c], v[x][c][0], v[x][c][1], v[x][c][2], v[x][c][3], hi[x][n][0], hi[x][n][1], T());
+#pragma unroll
+                        for (int c = 0; c < D / 16; ++c)
+                            paged_mma(acc[n][c], v[x][c][0], v[x][c][1], v[x][c][2], v[x][c][3], lo[x][n][0], lo[x][n][1], T());
                     }
-                }
             });
         __syncwarp();   // the ring has been read
         float* out = reinterpret_cast<float*>(ring);
@@ -357,48 +454,66 @@ template <typename T, int LPK, int VPL, int HB> struct PagedFma {
     static_assert(HEADS * D * 4 <= RING, "a warp's sums fit its ring");
     static __device__ __forceinline__ float read(const float* s) { return *s; }
 
-    static __device__ __forceinline__ void fetch(const PagedArgs& a, const T* base, const int64_t* off, int count, uint32_t ring_at, int i0, int stage)
+    static __device__ __forceinline__ void fetch(const PagedArgs& a, const T* base, PagedCursor<TILE>& cursor, uint32_t ring_at, int n, int stage)
     {
         const int lane = threadIdx.x & 31, part = lane & (LPK - 1), sub = lane / LPK;
+        bool whole;
+        const int64_t* off = cursor.tile(n, &whole);
+        const uint32_t to = ring_at + stage * STAGE + lane * 16;
+        const uint8_t* from = (const uint8_t*)(base + part * N);
+        if (whole && a.d.d == D) {
 #pragma unroll
-        for (int k = 0; k < U; ++k) {
-            const int i = i0 + k * SUB + sub;
-            const int64_t at = i < count ? off[i] : -1;
+            for (int k = 0; k < U; ++k)
 #pragma unroll
-            for (int v = 0; v < VPL; ++v) {
-                const int c = (v * LPK + part) * N;
-                const bool valid = at >= 0 && c < a.d.d;
-                paged_copy(ring_at + stage * STAGE + (k * VPL + v) * 512 + lane * 16, valid ? base + at + c : base, valid);
-            }
+                for (int v = 0; v < VPL; ++v) paged_copy(to + (k * VPL + v) * 512, from + off[k * SUB + sub] + v * (LPK * 16));
+        } else {
+#pragma unroll
+            for (int k = 0; k < U; ++k)
+#pragma unroll
+                for (int v = 0; v < VPL; ++v) {
+                    const bool has = (v * LPK + part) * N < a.d.d;
+                    paged_copy_or_zero(to + (k * VPL + v) * 512, has ? from + v * (LPK * 16) : (const uint8_t*)base, has ? off[k * SUB + sub] : PAGED_NONE);
+                }
         }
+    }
+    static __device__ __forceinline__ void take(Vec16<T> (&x)[U][VPL], const unsigned char* ring, int stage)
+    {
+        const uint4* tile = reinterpret_cast<const uint4*>(ring + stage * STAGE) + (threadIdx.x & 31);
+#pragma unroll
+        for (int k = 0; k < U; ++k)
+#pragma unroll
+            for (int v = 0; v < VPL; ++v) x[k][v].raw = tile[(k * VPL + v) * 32];
     }
 
     template <typename Put>
-    static __device__ __forceinline__ void scores(const PagedArgs& a, const T* Q, int nh, const T* K, const int64_t* off, int count, unsigned char* ring,
+    static __device__ __forceinline__ void scores(const PagedArgs& a, const T* Q, int nh, const T* K, const PagedTokens& tok, unsigned char* ring, int64_t* offsets,
                                                   float* warp_max, Put put)
     {
         using Sums = PagedSums<HB * U, LPK>;   // sum number k * HB + h: token k, head h
         const int lane = threadIdx.x & 31, part = lane & (LPK - 1), sub = lane / LPK;
+        const int count = tok.count;
         const uint32_t ring_at = nm_smem_u32(ring);
+        PagedCursor<TILE> cursor(a, tok, offsets);
         const int sum0 = Sums::first(part);
+        Vec16<T> x[U][VPL];
         float q[HB][VPL][N], m[Sums::LEFT];
         paged_pipeline<STAGES, TILE>(
-            count, [&](int i0, int stage) { fetch(a, K, off, count, ring_at, i0, stage); },
+            count, [&](int n, int stage) { fetch(a, K, cursor, ring_at, n, stage); },
             [&] {
 #pragma unroll
                 for (int h = 0; h < HB; ++h)
 #pragma unroll
                     for (int v = 0; v < VPL; ++v) {
                         const int c = (v * LPK + part) * N;
-                        Vec16<T> x;
-                        x.raw = h < nh && c < a.d.d ? *reinterpret_cast<const uint4*>(Q + h * a.d.d + c) : make_uint4(0, 0, 0, 0);
-                        x.get(q[h][v]);
+                        Vec16<T> y;
+                        y.raw = h < nh && c < a.d.d ? *reinterpret_cast<const uint4*>(Q + h * a.d.d + c) : make_uint4(0, 0, 0, 0);
+                        y.get(q[h][v]);
                     }
 #pragma unroll
                 for (int i = 0; i < Sums::LEFT; ++i) m[i] = -INFINITY;
             },
-            [&](int i0, int stage) {
-                const uint4* tile = reinterpret_cast<const uint4*>(ring + stage * STAGE) + lane;
+            [&](int stage) { take(x, ring, stage); },
+            [&](int i0) {
                 float dot[HB * U];
 #pragma unroll
                 for (int k = 0; k < U; ++k) {
@@ -406,10 +521,8 @@ template <typename T, int LPK, int VPL, int HB> struct PagedFma {
                     for (int h = 0; h < HB; ++h) dot[k * HB + h] = 0.f;
 #pragma unroll
                     for (int v = 0; v < VPL; ++v) {
-                        Vec16<T> x;
-                        x.raw = tile[(k * VPL + v) * 32];
                         float f[N];
-                        x.get(f);
+                        x[k][v].get(f);
 #pragma unroll
                         for (int h = 0; h < HB; ++h)
 #pragma unroll
@@ -440,21 +553,31 @@ template <typename T, int LPK, int VPL, int HB> struct PagedFma {
     }
 
     template <typename Max, typename Get>
-    static __device__ __forceinline__ void values(const PagedArgs& a, int nh, const T* V, const int64_t* off, int count, PagedExp exp, unsigned char* ring,
+    static __device__ __forceinline__ void values(const PagedArgs& a, int nh, const T* V, const PagedTokens& tok, PagedExp exp, unsigned char* ring, int64_t* offsets,
                                                   float* warp_sum, Max maxima, Get get)
     {
         const int lane = threadIdx.x & 31, part = lane & (LPK - 1), sub = lane / LPK;
+        const int count = tok.count;
         const uint32_t ring_at = nm_smem_u32(ring);
+        PagedCursor<TILE> cursor(a, tok, offsets);
         constexpr int TH = U * HB;   // a token's exponentials are shared by its lanes: lane `part` computes number part, part + LPK, ...
         constexpr int MINE = (TH + LPK - 1) / LPK;
-        float acc[HB][VPL][N], sum[MINE], m[MINE];
+        Vec16<T> x[U][VPL];
+        float acc[HB][VPL][N], sum[MINE], m[MINE], next[MINE];   // next: scores of the next tile
+        auto look = [&](int i0) {
+#pragma unroll
+            for (int l = 0; l < MINE; ++l) {
+                const int y = l * LPK + part, h = y % HB, i = i0 + y / HB * SUB + sub;
+                next[l] = y < TH && h < nh && i < count ? get(h, i) : 0.f;
+            }
+        };
         paged_pipeline<STAGES, TILE>(
-            count, [&](int i0, int stage) { fetch(a, V, off, count, ring_at, i0, stage); },
+            count, [&](int n, int stage) { fetch(a, V, cursor, ring_at, n, stage); },
             [&] {
-                const float* x = maxima();
+                const float* max = maxima();
 #pragma unroll
                 for (int l = 0; l < MINE; ++l) {
-                    m[l] = x[(l * LPK + part) % HB];
+                    m[l] = max[(l * LPK + part) % HB];
                     sum[l] = 0.f;
                 }
 #pragma unroll
@@ -463,16 +586,18 @@ template <typename T, int LPK, int VPL, int HB> struct PagedFma {
                     for (int v = 0; v < VPL; ++v)
 #pragma unroll
                         for (int e = 0; e < N; ++e) acc[h][v][e] = 0.f;
+                look((threadIdx.x >> 5) * TILE);
             },
-            [&](int i0, int stage) {
-                const uint4* tile = reinterpret_cast<const uint4*>(ring + stage * STAGE) + lane;
+            [&](int stage) { take(x, ring, stage); },
+            [&](int i0) {
                 float mine[MINE];
 #pragma unroll
                 for (int l = 0; l < MINE; ++l) {
-                    const int x = l * LPK + part, h = x % HB, i = i0 + x / HB * SUB + sub;
-                    mine[l] = x < TH && h < nh && i < count ? exp(get(h, i) - m[l]) : 0.f;
+                    const int y = l * LPK + part, h = y % HB, i = i0 + y / HB * SUB + sub;
+                    mine[l] = y < TH && h < nh && i < count ? exp(next[l] - m[l]) : 0.f;
                     sum[l] += mine[l];
                 }
+                look(i0 + PAGED_WARPS * TILE);
 #pragma unroll
                 for (int k = 0; k < U; ++k) {
                     float e[HB];
@@ -481,10 +606,8 @@ template <typename T, int LPK, int VPL, int HB> struct PagedFma {
                         e[h] = __shfl_sync(0xffffffffu, mine[(k * HB + h) / LPK], (lane & ~(LPK - 1)) | ((k * HB + h) % LPK));
 #pragma unroll
                     for (int v = 0; v < VPL; ++v) {
-                        Vec16<T> x;
-                        x.raw = tile[(k * VPL + v) * 32];
                         float f[N];
-                        x.get(f);
+                        x[k][v].get(f);
 #pragma unroll
                         for (int h = 0; h < HB; ++h)
 #pragma unroll
@@ -533,20 +656,20 @@ template <class Core> __device__ __forceinline__ PagedUnit paged_unit(const Page
 }
 // scores of a block: rows of this many floats (8 beyond a multiple of 32: eight heads' pairs lie in different banks)
 __host__ __device__ constexpr int paged_pitch(int span) { return (span + 31) / 32 * 32 + 8; }
-template <class Core> constexpr size_t paged_split_bytes(int span) { return (size_t)PAGED_WARPS * Core::RING + (size_t)span * 8; }
-template <class Core> constexpr size_t paged_fused_bytes(int span)
-{
-    return paged_split_bytes<Core>(span) + (size_t)Core::HEADS * paged_pitch(span) * 4;
-}
+// blocks of an SM: rings of 64 KB leave room for two
+constexpr int paged_blocks(int ring) { return ring > 8192 ? 1 : 2; }
+constexpr size_t PAGED_OFFSETS = PAGED_WARPS * 64 * 8;   // the cursors' rounds
+template <class Core> constexpr size_t paged_split_bytes() { return (size_t)PAGED_WARPS * Core::RING + PAGED_OFFSETS; }
+template <class Core> constexpr size_t paged_fused_bytes(int span) { return paged_split_bytes<Core>() + (size_t)Core::HEADS * paged_pitch(span) * 4; }
 
 #define NM_PAGED_EXP_TABLE()                                                                             \
     __shared__ float2 s_exp[NM_MAX_SEGMENTS];                                                            \
     for (int i = threadIdx.x; i < a.exp_tab->n; i += PAGED_THREADS) s_exp[i] = a.exp_tab->kb[i];         \
-    const PagedExp exp = {s_exp, a.exp_tab->inv_h, a.exp_tab->off, (float)(a.exp_tab->n - 1)}
+    const PagedExp exp = {nm_smem_u32(s_exp) - (0x4B400000u << 3), a.exp_tab->inv_h, a.exp_tab->off, (float)(a.exp_tab->n - 1)}
 
 // One launch: a cluster per unit, its blocks sharing the row's tokens evenly.
 template <class Core>
-__global__ void __launch_bounds__(PAGED_THREADS, 2) paged_fused_kernel(const PagedArgs a)
+__global__ void __launch_bounds__(PAGED_THREADS, paged_blocks(Core::RING)) paged_fused_kernel(const PagedArgs a)
 {
     using T = typename Core::Elem;
     extern __shared__ __align__(128) unsigned char paged_smem[];
@@ -561,17 +684,16 @@ __global__ void __launch_bounds__(PAGED_THREADS, 2) paged_fused_kernel(const Pag
     nm_grid_dependency_wait();
     const int len = paged_length(a, u.b);
     if (len < 0) return;   // the whole cluster
-    const int per = ((len + (int)ctas - 1) / (int)ctas + 15) / 16 * 16, first = min(len, rank * per), count = min(len - first, per);
+    const int per = ((len + (int)ctas - 1) / (int)ctas + 31) / 32 * 32, first = min(len, rank * per);
+    const PagedTokens tok = {a.d.block_tables + (int64_t)u.b * a.d.ld_tables, first, min(len - first, per)};
     const int pitch = paged_pitch(a.span), warp = threadIdx.x >> 5;
     unsigned char* ring = paged_smem + warp * Core::RING;
-    int64_t* off = reinterpret_cast<int64_t*>(paged_smem + PAGED_WARPS * Core::RING);
-    float* sc = reinterpret_cast<float*>(off + a.span);
-    paged_offsets(a, u.b, first, count, off);
-    __syncthreads();
+    int64_t* offsets = reinterpret_cast<int64_t*>(paged_smem + PAGED_WARPS * Core::RING) + warp * 64;
+    float* sc = reinterpret_cast<float*>(paged_smem + PAGED_WARPS * Core::RING + PAGED_OFFSETS);
     Core::scores(a, (const T*)a.d.Q + (int64_t)u.b * a.d.ld_q + (int64_t)u.h0 * a.d.d, u.nh, (const T*)a.d.k_cache + (int64_t)u.kv * a.d.stride_head,
-                 off, count, ring, s_max[warp], [&](int h, int i, float s) { sc[h * pitch + i] = s; });
+                 tok, ring, offsets, s_max[warp], [&](int h, int i, float s) { sc[h * pitch + i] = s; });
     Core::values(
-        a, u.nh, (const T*)a.d.v_cache + (int64_t)u.kv * a.d.stride_head, off, count, exp, ring, s_sum[warp],
+        a, u.nh, (const T*)a.d.v_cache + (int64_t)u.kv * a.d.stride_head, tok, exp, ring, offsets, s_sum[warp],
         [&] {   // the row's maxima
             __syncthreads();
             if (threadIdx.x < Core::HEADS) {
@@ -628,119 +750,276 @@ __global__ void __launch_bounds__(PAGED_THREADS, 2) paged_fused_kernel(const Pag
     if (ctas > 1) nm_cluster_sync();   // no block leaves while another reads its shared memory
 }
 
+// Split form.  All requests' units lie one after another, every unit's tokens as whole 32s; block i has positions [i * share, (i + 1) * share).
+// Its part of one unit is a segment.  A unit that lies in several blocks has one segment in each: the block's head segment where the
+// unit covers the block's first position, its tail segment otherwise, so a block has room for the sums of two.
+struct PagedShare {
+    int64_t share, pos, end, row0;   // the block's positions still to do; where the current request's first unit begins
+    int b, len;                      // the current request
+};
+__device__ __forceinline__ int paged_len32(int len) { return (len + 31) & ~31; }
+
+// Length of request b for the shares: 0 where it is outside what the call was made for.
+__device__ __forceinline__ int paged_length_or_0(const PagedArgs& a, int b)
+{
+    const int n = a.d.lengths[b];
+    return n < 0 || n > a.d.max_len ? 0 : n;
+}
+
+// The block's share: two passes over the lengths, 256 requests at a time.
+__device__ __forceinline__ PagedShare paged_share(const PagedArgs& a, int units)
+{
+    __shared__ int64_t s_warp[PAGED_WARPS], s_row0;
+    __shared__ int s_b;
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    int64_t mine = 0;
+    for (int b = tid; b < a.d.B; b += PAGED_THREADS) mine += paged_len32(paged_length_or_0(a, b));
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) mine += __shfl_xor_sync(0xffffffffu, mine, o);
+    if (lane == 0) s_warp[warp] = mine;
+    if (tid == 0) s_b = -1;
+    __syncthreads();
+    int64_t total = 0;
+#pragma unroll
+    for (int w = 0; w < PAGED_WARPS; ++w) total += s_warp[w];
+    total *= units;
+    PagedShare s;
+    s.share = ((total + gridDim.x - 1) / gridDim.x + 31) / 32 * 32;
+    if (s.share < a.span) s.share = a.span;
+    s.pos = (int64_t)blockIdx.x * s.share;
+    s.end = s.pos + s.share < total ? s.pos + s.share : total;
+    s.b = s.len = 0;
+    s.row0 = 0;
+    if (s.pos >= s.end) return s;
+    int64_t before = 0;   // of the requests of earlier turns
+    for (int b0 = 0; b0 < a.d.B; b0 += PAGED_THREADS) {
+        const int b = b0 + tid;
+        const int64_t own = b < a.d.B ? (int64_t)paged_len32(paged_length_or_0(a, b)) * units : 0;
+        int64_t x = own;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const int64_t y = __shfl_up_sync(0xffffffffu, x, o);
+            if (lane >= o) x += y;
+        }
+        __syncthreads();
+        if (lane == 31) s_warp[warp] = x;
+        __syncthreads();
+        int64_t at = before;
+        for (int w = 0; w < PAGED_WARPS; ++w) {
+            if (w < warp) at += s_warp[w];
+            before += s_warp[w];
+        }
+        at += x - own;
+        if (at <= s.pos && s.pos < at + own) {   // one thread at most
+            s_b = b;
+            s_row0 = at;
+        }
+        if (before > s.pos) break;
+    }
+    __syncthreads();
+    s.b = s_b;
+    s.row0 = s_row0;
+    s.len = paged_length_or_0(a, s.b);
+    return s;
+}
+struct PagedSegment {
+    int b, unit, first, count;   // request, unit of it, tokens
+    int64_t from;                // the unit's first position
+    bool whole;                  // the unit lies in this block alone
+};
+// The next segment of the block; false when there is none.
+__device__ __forceinline__ bool paged_next(const PagedArgs& a, PagedShare& s, int units, PagedSegment* g)
+{
+    if (s.pos >= s.end) return false;
+    int len32 = paged_len32(s.len);
+    while (s.pos >= s.row0 + (int64_t)len32 * units) {   // the next request that has tokens
+        s.row0 += (int64_t)len32 * units;
+        s.len = paged_length_or_0(a, ++s.b);
+        len32 = paged_len32(s.len);
+    }
+    const int64_t local = s.pos - s.row0;
+    g->b = s.b;
+    g->unit = (int)(local / len32);
+    g->from = s.row0 + (int64_t)g->unit * len32;
+    g->first = (int)(s.pos - g->from);
+    const int64_t stop = g->from + len32 < s.end ? g->from + len32 : s.end;
+    g->count = min(s.len, (int)(stop - g->from)) - g->first;
+    g->whole = g->first == 0 && stop == g->from + len32;
+    s.pos = stop;
+    return true;
+}
+// place of block c's sums of the unit that begins at `from`
+__device__ __forceinline__ int64_t paged_place(int64_t from, int64_t share, int64_t c) { return 2 * c + (from <= c * share ? 0 : 1); }
+
 template <class Core>
-__global__ void __launch_bounds__(PAGED_THREADS, 2) paged_scores_kernel(const PagedArgs a)
+__global__ void __launch_bounds__(PAGED_THREADS, paged_blocks(Core::RING)) paged_scores_kernel(const PagedArgs a)
 {
     using T = typename Core::Elem;
     extern __shared__ __align__(128) unsigned char paged_smem[];
     __shared__ float s_max[PAGED_WARPS][Core::HEADS];
-    const int span = (int)(blockIdx.x % a.spans), first = span * a.span;
-    const PagedUnit u = paged_unit<Core>(a, blockIdx.x / a.spans);
-    nm_grid_launch_dependents();
-    nm_grid_dependency_wait();
-    const int len = paged_length(a, u.b);
-    if (first >= len) return;
-    const int count = min(len - first, a.span);
-    unsigned char* ring = paged_smem + (threadIdx.x >> 5) * Core::RING;
-    int64_t* off = reinterpret_cast<int64_t*>(paged_smem + PAGED_WARPS * Core::RING);
-    paged_offsets(a, u.b, first, count, off);
-    __syncthreads();
-    float* sc = a.scores + ((int64_t)u.b * a.d.heads + u.h0) * a.row + first;
-    Core::scores(a, (const T*)a.d.Q + (int64_t)u.b * a.d.ld_q + (int64_t)u.h0 * a.d.d, u.nh, (const T*)a.d.k_cache + (int64_t)u.kv * a.d.stride_head,
-                 off, count, ring, s_max[threadIdx.x >> 5], [&](int h, int i, float s) {
-                     if (h < u.nh) sc[h * a.row + i] = s;
-                 });
-    __syncthreads();
-    if ((int)threadIdx.x < u.nh) {
-        float x = s_max[0][threadIdx.x];
-        for (int w = 1; w < PAGED_WARPS; ++w) x = fmaxf(x, s_max[w][threadIdx.x]);
-        a.maxima[((int64_t)u.b * a.d.heads + u.h0 + threadIdx.x) * a.spans + span] = x;
-    }
-}
-
-template <class Core>
-__global__ void __launch_bounds__(PAGED_THREADS, 2) paged_values_kernel(const PagedArgs a)
-{
-    using T = typename Core::Elem;
-    extern __shared__ __align__(128) unsigned char paged_smem[];
-    __shared__ float s_m[Core::HEADS], s_sum[PAGED_WARPS][Core::HEADS];
-    NM_PAGED_EXP_TABLE();
-    const int span = (int)(blockIdx.x % a.spans), first = span * a.span, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const PagedUnit u = paged_unit<Core>(a, blockIdx.x / a.spans);
-    nm_grid_launch_dependents();
-    nm_grid_dependency_wait();
-    const int len = paged_length(a, u.b);
-    if (first >= len) return;
-    const int count = min(len - first, a.span), used = (len + a.span - 1) / a.span;
+    const int units = a.d.kv_heads * a.blocks_per_head, warp = threadIdx.x >> 5;
     unsigned char* ring = paged_smem + warp * Core::RING;
-    int64_t* off = reinterpret_cast<int64_t*>(paged_smem + PAGED_WARPS * Core::RING);
-    paged_offsets(a, u.b, first, count, off);
-    const int64_t head0 = (int64_t)u.b * a.d.heads + u.h0;
-    for (int h = warp; h < Core::HEADS; h += PAGED_WARPS) {
-        float m = -INFINITY;
-        if (h < u.nh)
-            for (int i = lane; i < used; i += 32) m = fmaxf(m, a.maxima[(head0 + h) * a.spans + i]);
-#pragma unroll
-        for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
-        if (lane == 0) s_m[h] = m;
-    }
-    __syncthreads();
-    const float* sc = a.scores + head0 * a.row + first;
-    Core::values(a, u.nh, (const T*)a.d.v_cache + (int64_t)u.kv * a.d.stride_head, off, count, exp, ring, s_sum[warp], [&] { return (const float*)s_m; },
-                 [&](int h, int i) { return Core::read(sc + h * a.row + i); });
-    __syncthreads();
-    for (int x = threadIdx.x; x < u.nh * Core::D; x += PAGED_THREADS) {
-        const int h = x / Core::D, c = x - h * Core::D;
-        if (c >= a.d.d) continue;
-        const float* out = reinterpret_cast<const float*>(paged_smem);
-        float o = out[x], s = s_sum[0][h];
-        for (int w = 1; w < PAGED_WARPS; ++w) {
-            o += out[w * (Core::RING / 4) + x];
-            s += s_sum[w][h];
+    int64_t* offsets = reinterpret_cast<int64_t*>(paged_smem + PAGED_WARPS * Core::RING) + warp * 64;
+    nm_grid_dependency_wait();
+    nm_grid_launch_dependents();   // what came before this launch is complete for the next one too
+    if (threadIdx.x == 0) a.tickets[blockIdx.x] = 0;
+    PagedShare share = paged_share(a, units);
+    PagedSegment g;
+    while (paged_next(a, share, units, &g)) {
+        const PagedUnit u = paged_unit<Core>(a, (int64_t)g.b * units + g.unit);
+        const PagedTokens tok = {a.d.block_tables + (int64_t)u.b * a.d.ld_tables, g.first, g.count};
+        float* sc = a.scores + ((int64_t)u.b * a.d.heads + u.h0) * a.row + g.first;
+        Core::scores(a, (const T*)a.d.Q + (int64_t)u.b * a.d.ld_q + (int64_t)u.h0 * a.d.d, u.nh, (const T*)a.d.k_cache + (int64_t)u.kv * a.d.stride_head,
+                     tok, ring, offsets, s_max[warp], [&](int h, int i, float s) {
+                         if (h < u.nh) sc[h * a.row + i] = s;
+                     });
+        __syncthreads();
+        if ((int)threadIdx.x < u.nh) {
+            float x = s_max[0][threadIdx.x];
+            for (int w = 1; w < PAGED_WARPS; ++w) x = fmaxf(x, s_max[w][threadIdx.x]);
+            if (g.whole) a.maxima[(int64_t)u.b * a.d.heads + u.h0 + threadIdx.x] = x;
+            else a.part_max[paged_place(g.from, share.share, blockIdx.x) * Core::HEADS + threadIdx.x] = x;
         }
-        const int64_t row = (head0 + h) * a.spans + span;
-        a.outs[row * a.d.d + c] = o;
-        if (c == 0) a.sums[row] = s;
+        __syncthreads();
     }
 }
 
-// A block per request and head: four warps take every fourth span, a lane four channels of a span.
-constexpr int JOIN_WARPS = 4;
-template <typename T>
-__global__ void __launch_bounds__(JOIN_WARPS * 32) paged_join_kernel(const PagedArgs a)
+__host__ __device__ constexpr int paged_part_floats(int heads, int d) { return heads * d + (heads + 3) / 4 * 4; }   // [head][channel], then the row sums
+
+// The result of a unit that blocks c0..c1 have: groups of threads take every so manieth block, four channels a thread, eight blocks'
+// loads in flight; then the groups' sums are added.  (One thread after another through the blocks, each load waiting for the
+// last: 25 us for the 37 blocks of a unit.)
+template <class Core, typename T>
+__device__ __forceinline__ void paged_join(const PagedArgs& a, int nh, int64_t from, int64_t share, int64_t c0, int64_t c1, float* smem, T* result)
 {
-    __shared__ float s_out[JOIN_WARPS][256], s_sum[JOIN_WARPS];
-    const int64_t bh = blockIdx.x;
-    const int b = (int)(bh / a.d.heads), h = (int)(bh - (int64_t)b * a.d.heads), lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    nm_grid_launch_dependents();
-    nm_grid_dependency_wait();
-    const int len = paged_length(a, b);
-    if (len < 0) return;
-    const int used = (len + a.span - 1) / a.span;
-    float s = 0.f;
-    for (int i = warp * 32 + lane; i < used; i += JOIN_WARPS * 32) s += a.sums[bh * a.spans + i];
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
-    if (lane == 0) s_sum[warp] = s;
-    for (int c = lane * 4; c < a.d.d; c += 128) {
+    const int d4 = a.d.d / 4, items = nh * d4, groups = items < PAGED_THREADS ? PAGED_THREADS / items : 1, n = (int)(c1 - c0) + 1;
+    const int stride = paged_part_floats(Core::HEADS, a.d.d);
+    float4* s_out = reinterpret_cast<float4*>(smem);                       // [group][item]
+    float* s_sum = smem + groups * items * 4;                              // [group][item]
+    for (int y = threadIdx.x; y < groups * items; y += PAGED_THREADS) {
+        const int x = y % items, h = x / d4;
         float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 4
-        for (int i = warp; i < used; i += JOIN_WARPS) {
-            const float4 v = *reinterpret_cast<const float4*>(a.outs + (bh * a.spans + i) * a.d.d + c);
+        float s = 0.f;
+#pragma unroll 8
+        for (int i = y / items; i < n; i += groups) {
+            const float* p = a.parts + paged_place(from, share, c0 + i) * stride;
+            const float4 v = __ldcg(reinterpret_cast<const float4*>(p) + x);
             o.x += v.x;
             o.y += v.y;
             o.z += v.z;
             o.w += v.w;
+            s += __ldcg(p + Core::HEADS * a.d.d + h);
         }
-        *reinterpret_cast<float4*>(&s_out[warp][c]) = o;
+        s_out[y] = o;
+        s_sum[y] = s;
     }
     __syncthreads();
-    s = s_sum[0] + s_sum[1] + s_sum[2] + s_sum[3];
-    const float r = paged_table(a.recip_tab, s);
-    for (int c = threadIdx.x; c < a.d.d; c += JOIN_WARPS * 32) {
-        const float o = s_out[0][c] + s_out[1][c] + s_out[2][c] + s_out[3][c];
-        ((T*)a.d.out)[(int64_t)b * a.d.ld_out + (int64_t)h * a.d.d + c] = NmType<T>::from_f(used ? o * r : 0.f);
+    for (int x = threadIdx.x; x < items; x += PAGED_THREADS) {
+        float4 o = s_out[x];
+        float s = s_sum[x];
+        for (int g = 1; g < groups; ++g) {
+            const float4 v = s_out[g * items + x];
+            o.x += v.x;
+            o.y += v.y;
+            o.z += v.z;
+            o.w += v.w;
+            s += s_sum[g * items + x];
+        }
+        const float r = paged_table(a.recip_tab, s);
+        result[x * 4] = NmType<T>::from_f(o.x * r);
+        result[x * 4 + 1] = NmType<T>::from_f(o.y * r);
+        result[x * 4 + 2] = NmType<T>::from_f(o.z * r);
+        result[x * 4 + 3] = NmType<T>::from_f(o.w * r);
     }
+}
+
+template <class Core>
+__global__ void __launch_bounds__(PAGED_THREADS, paged_blocks(Core::RING)) paged_values_kernel(const PagedArgs a)
+{
+    using T = typename Core::Elem;
+    extern __shared__ __align__(128) unsigned char paged_smem[];
+    __shared__ float s_m[Core::HEADS], s_sum[PAGED_WARPS][Core::HEADS];
+    __shared__ int s_last;
+    NM_PAGED_EXP_TABLE();
+    const int units = a.d.kv_heads * a.blocks_per_head, warp = threadIdx.x >> 5;
+    unsigned char* ring = paged_smem + warp * Core::RING;
+    int64_t* offsets = reinterpret_cast<int64_t*>(paged_smem + PAGED_WARPS * Core::RING) + warp * 64;
+    const float* out = reinterpret_cast<const float*>(paged_smem);
+    nm_grid_launch_dependents();
+    // Only the scores come from the launch before, which has let this one start once everything before it was complete: lengths,
+    // tables and the first values are read before it is done.
+    PagedShare share = paged_share(a, units);
+    bool waited = false;
+    for (int b = blockIdx.x; b < a.d.B; b += gridDim.x) {
+        const int n = a.d.lengths[b];
+        if (n < 0 || n > a.d.max_len) {
+            if (threadIdx.x == 0) atomicExch(a.status, (int)NM_ERR_SHAPE);
+        } else if (n == 0) {
+            if (!waited) nm_grid_dependency_wait();   // nothing is written before
+            waited = true;
+            for (int x = threadIdx.x; x < a.d.heads * a.d.d; x += PAGED_THREADS) ((T*)a.d.out)[(int64_t)b * a.d.ld_out + x] = NmType<T>::from_f(0.f);
+        }
+    }
+    PagedSegment g;
+    while (paged_next(a, share, units, &g)) {
+        const PagedUnit u = paged_unit<Core>(a, (int64_t)g.b * units + g.unit);
+        const PagedTokens tok = {a.d.block_tables + (int64_t)u.b * a.d.ld_tables, g.first, g.count};
+        const int64_t head0 = (int64_t)u.b * a.d.heads + u.h0;
+        const int64_t c0 = g.from / share.share, c1 = (g.from + paged_len32(share.len) - 1) / share.share;   // the unit's blocks
+        const float* sc = a.scores + head0 * a.row + g.first;
+        Core::values(
+            a, u.nh, (const T*)a.d.v_cache + (int64_t)u.kv * a.d.stride_head, tok, exp, ring, offsets, s_sum[warp],
+            [&] {
+                if (!waited) nm_grid_dependency_wait();
+                waited = true;
+                if (g.whole) {
+                    if ((int)threadIdx.x < Core::HEADS) s_m[threadIdx.x] = (int)threadIdx.x < u.nh ? a.maxima[head0 + threadIdx.x] : 0.f;
+                } else {
+                    const int lane = threadIdx.x & 31;
+                    for (int h = warp; h < Core::HEADS; h += PAGED_WARPS) {
+                        float m = -INFINITY;
+                        if (h < u.nh)
+                            for (int64_t c = c0 + lane; c <= c1; c += 32) m = fmaxf(m, a.part_max[paged_place(g.from, share.share, c) * Core::HEADS + h]);
+#pragma unroll
+                        for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+                        if (lane == 0) s_m[h] = m;
+                    }
+                }
+                __syncthreads();
+                return (const float*)s_m;
+            },
+            [&](int h, int i) { return Core::read(sc + h * a.row + i); });
+        __syncthreads();
+        T* result = (T*)a.d.out + (int64_t)u.b * a.d.ld_out + (int64_t)u.h0 * a.d.d;
+        float* part = a.parts + paged_place(g.from, share.share, blockIdx.x) * paged_part_floats(Core::HEADS, a.d.d);
+        for (int x = threadIdx.x; x < u.nh * Core::D; x += PAGED_THREADS) {
+            const int h = x / Core::D, c = x - h * Core::D;
+            if (c >= a.d.d) continue;
+            float o = out[x], s = s_sum[0][h];
+            for (int w = 1; w < PAGED_WARPS; ++w) {
+                o += out[w * (Core::RING / 4) + x];
+                s += s_sum[w][h];
+            }
+            if (g.whole) {
+                result[h * a.d.d + c] = NmType<T>::from_f(o * paged_table(a.recip_tab, s));
+            } else {
+                part[h * a.d.d + c] = o;
+                if (c == 0) part[Core::HEADS * a.d.d + h] = s;
+            }
+        }
+        if (!g.whole) {   // the unit's last block adds up what all of them left, in their order
+            __syncthreads();
+            if (threadIdx.x == 0) {
+                __threadfence();
+                s_last = atomicAdd(a.tickets + c0, 1) == (int)(c1 - c0);
+                __threadfence();
+            }
+            __syncthreads();
+            if (s_last) paged_join<Core>(a, u.nh, g.from, share.share, c0, c1, reinterpret_cast<float*>(paged_smem), result);
+        }
+        __syncthreads();   // the ring and the sums have been read
+    }
+    if (!waited) nm_grid_dependency_wait();   // a launch is not complete before the one it followed
 }
 
 // ---------------------------------------------------------------- host
@@ -754,48 +1033,44 @@ int paged_heads(const nm_attn_paged_desc* d, bool mma)
     if (mma) return group > 8 && d->d <= 128 ? 16 : 8;
     return group >= 8 ? 8 : group >= 4 ? 4 : group >= 2 ? 2 : 1;
 }
-// Tokens of a block of the fused form: offsets and scores take what rings of 64 KB leave of half an SM's shared memory.
-int paged_cap(int heads) { return (44 * 1024 - heads * 4 * 40) / (8 + heads * 4) / 16 * 16; }
+// Tokens of a block of the fused form: scores take what rings of 64 KB leave of half an SM's shared memory.
+int paged_cap(int heads) { return (40 * 1024 - heads * 4 * 40) / (heads * 4) / 32 * 32; }
 bool paged_mma_supported(const nm_attn_paged_desc* d) { return d->dtype != NM_F32 && (d->d == 64 || d->d == 96 || d->d == 128 || d->d == 256); }
 
 struct PagedLayout {
     bool mma, fused;
-    int heads, blocks_per_head, ctas, span, spans;
-    int64_t units, row;
-    size_t scores, maxima, sums, outs, total;
+    int heads, blocks_per_head, ctas, span;
+    int64_t units, row, blocks;
+    size_t scores, maxima, part_max, parts, tickets, total;
 };
 PagedLayout layout_of(const nm_attn_paged_desc* d)
 {
-    PagedLayout l;
+    PagedLayout l = PagedLayout();
     const int group = d->heads / d->kv_heads;
     l.mma = paged_mma_supported(d);
     l.heads = paged_heads(d, l.mma);
     l.blocks_per_head = (group + l.heads - 1) / l.heads;
     l.units = (int64_t)d->B * d->kv_heads * l.blocks_per_head;
-    l.scores = l.maxima = l.sums = l.outs = l.total = 0;
-    l.row = 0;
-    l.spans = 1;
     const int cap = paged_cap(l.heads);
-    l.fused = d->max_len <= 8 * cap;
+    int ctas = 1;
+    while (ctas < 8 && ((d->max_len + ctas - 1) / ctas > cap || (l.units * ctas * 2 <= 2 * PAGED_SMS && d->max_len > ctas * 128))) ctas *= 2;
+    l.fused = d->max_len <= ctas * cap && l.units * ctas <= 2 * PAGED_SMS;
     if (l.fused) {
-        int ctas = 1;
-        while (ctas < 8 && ((d->max_len + ctas - 1) / ctas > cap || (l.units * ctas * 2 <= 2 * PAGED_SMS && d->max_len > ctas * 128))) ctas *= 2;
         l.ctas = ctas;
-        l.span = ((d->max_len + ctas - 1) / ctas + 15) / 16 * 16;
+        l.span = ((d->max_len + ctas - 1) / ctas + 31) / 32 * 32;
+        l.blocks = l.units * ctas;
         return l;
     }
     l.ctas = 1;
-    // spans of whole 128 tokens, as many as make twelve blocks per SM
-    const int64_t tokens = (l.units * d->max_len + PAGED_SMS * 12 - 1) / (PAGED_SMS * 12);
-    l.span = (int)(((tokens > 2048 ? 2048 : tokens) + 127) / 128 * 128);
-    l.spans = (int)(((int64_t)d->max_len + l.span - 1) / l.span);
+    l.span = 256;
+    l.blocks = PAGED_SMS * (l.mma && d->d == 256 ? 1 : 2);   // one wave
     l.row = ((int64_t)d->max_len + 31) / 32 * 32;
-    const size_t bh = (size_t)d->B * d->heads;
     auto take = [&l](size_t bytes) { const size_t at = l.total; l.total += (bytes + 255) / 256 * 256; return at; };
-    l.scores = take(bh * l.row * 4);
-    l.maxima = take(bh * l.spans * 4);
-    l.sums = take(bh * l.spans * 4);
-    l.outs = take(bh * l.spans * d->d * 4);
+    l.scores = take((size_t)d->B * d->heads * l.row * 4);
+    l.maxima = take((size_t)d->B * d->heads * 4);
+    l.part_max = take((size_t)l.blocks * 2 * l.heads * 4);
+    l.parts = take((size_t)l.blocks * 2 * paged_part_floats(l.heads, d->d) * 4);
+    l.tickets = take((size_t)l.blocks * 4);
     return l;
 }
 
@@ -815,12 +1090,9 @@ nm_status launch(nm_ctx* ctx, const PagedArgs& a, const PagedLayout& l, cudaStre
 {
     using T = typename Core::Elem;
     const double bytes = (double)a.d.B * a.d.max_len * a.d.kv_heads * a.d.d * sizeof(T);
-    if (l.fused) return paged_launch(ctx, paged_fused_kernel<Core>, a, l.units * l.ctas, PAGED_THREADS, paged_fused_bytes<Core>(l.span), l.ctas, 2 * bytes, st);
-    nm_status s = paged_launch(ctx, paged_scores_kernel<Core>, a, l.units * l.spans, PAGED_THREADS, paged_split_bytes<Core>(l.span), 1, bytes, st);
-    if (s != NM_OK) return s;
-    s = paged_launch(ctx, paged_values_kernel<Core>, a, l.units * l.spans, PAGED_THREADS, paged_split_bytes<Core>(l.span), 1, bytes, st);
-    if (s != NM_OK) return s;
-    return paged_launch(ctx, paged_join_kernel<T>, a, (int64_t)a.d.B * a.d.heads, JOIN_WARPS * 32, 0, 1, 0.0, st);
+    if (l.fused) return paged_launch(ctx, paged_fused_kernel<Core>, a, l.blocks, PAGED_THREADS, paged_fused_bytes<Core>(l.span), l.ctas, 2 * bytes, st);
+    const nm_status s = paged_launch(ctx, paged_scores_kernel<Core>, a, l.blocks, PAGED_THREADS, paged_split_bytes<Core>(), 1, bytes, st);
+    return s != NM_OK ? s : paged_launch(ctx, paged_values_kernel<Core>, a, l.blocks, PAGED_THREADS, paged_split_bytes<Core>(), 1, bytes, st);
 }
 
 template <typename T>
@@ -868,12 +1140,23 @@ nm_status nm_launch_attention_paged(nm_ctx* ctx, const nm_attn_paged_desc* d, vo
     a.group = d->heads / d->kv_heads;
     a.blocks_per_head = l.blocks_per_head;
     a.span = l.span;
-    a.spans = l.spans;
+    const int es = (int)nm_dtype_size(d->dtype);
+    a.page_bytes = d->stride_page * es;
+    a.token_bytes = d->stride_token * es;
+    a.div_mul = a.div_shift = 0;
+    if (d->page_size > 1) {   // 2^(31 + l) / page_size rounded up, l = ceil(log2(page_size)): right for all numbers of 31 bits
+        int l = 1;
+        while (((int64_t)1 << l) < d->page_size) ++l;
+        a.div_mul = (uint32_t)(((uint64_t)1 << (31 + l)) / (uint32_t)d->page_size + 1);
+        a.div_shift = (uint32_t)(l - 1);
+    }
     a.row = l.row;
-    a.scores = (float*)((uint8_t*)workspace + l.scores);
-    a.maxima = (float*)((uint8_t*)workspace + l.maxima);
-    a.sums = (float*)((uint8_t*)workspace + l.sums);
-    a.outs = (float*)((uint8_t*)workspace + l.outs);
+    uint8_t* ws = (uint8_t*)workspace;
+    a.scores = (float*)(ws + l.scores);
+    a.maxima = (float*)(ws + l.maxima);
+    a.part_max = (float*)(ws + l.part_max);
+    a.parts = (float*)(ws + l.parts);
+    a.tickets = (int*)(ws + l.tickets);
     switch (d->dtype) {
     case NM_F32: return dispatch<float>(ctx, a, l, st);
     case NM_BF16: return dispatch<__nv_bfloat16>(ctx, a, l, st);
