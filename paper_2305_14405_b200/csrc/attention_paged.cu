@@ -673,7 +673,7 @@ __global__ void __launch_bounds__(PAGED_THREADS, paged_blocks(Core::RING)) paged
 {
     using T = typename Core::Elem;
     extern __shared__ __align__(128) unsigned char paged_smem[];
-    __shared__ float s_max[PAGED_WARPS][Core::HEADS], s_cluster_max[8][Core::HEADS], s_row_max[Core::HEADS];
+    __shared__ float s_max[PAGED_WARPS][Core::HEADS], s_block_max[Core::HEADS], s_row_max[Core::HEADS];
     __shared__ float s_sum[PAGED_WARPS][Core::HEADS], s_block_sum[Core::HEADS];
     NM_PAGED_EXP_TABLE();
     uint32_t ctas;
@@ -699,19 +699,18 @@ __global__ void __launch_bounds__(PAGED_THREADS, paged_blocks(Core::RING)) paged
             if (threadIdx.x < Core::HEADS) {
                 float x = s_max[0][threadIdx.x];
                 for (int w = 1; w < PAGED_WARPS; ++w) x = fmaxf(x, s_max[w][threadIdx.x]);
-                if (ctas == 1) {
-                    s_row_max[threadIdx.x] = x;
-                } else {
-                    const uint32_t at = nm_smem_u32(&s_cluster_max[rank][threadIdx.x]);
-                    for (uint32_t c = 0; c < ctas; ++c)
-                        asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(nm_mapa(at, c)), "f"(x) : "memory");
-                }
+                s_block_max[threadIdx.x] = x;
+                if (ctas == 1) s_row_max[threadIdx.x] = x;
             }
-            if (ctas > 1) {
+            if (ctas > 1) {   // the other blocks' maxima are read once all of them have come this far
                 nm_cluster_sync();
                 if (threadIdx.x < Core::HEADS) {
-                    float x = s_cluster_max[0][threadIdx.x];
-                    for (uint32_t c = 1; c < ctas; ++c) x = fmaxf(x, s_cluster_max[c][threadIdx.x]);
+                    float x = -INFINITY;
+                    for (uint32_t r = 0; r < ctas; ++r) {
+                        float y;
+                        asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(y) : "r"(nm_mapa(nm_smem_u32(&s_block_max[threadIdx.x]), r)) : "memory");
+                        x = fmaxf(x, y);
+                    }
                     s_row_max[threadIdx.x] = x;
                 }
             }
@@ -1054,7 +1053,7 @@ PagedLayout layout_of(const nm_attn_paged_desc* d)
     const int cap = paged_cap(l.heads);
     int ctas = 1;
     while (ctas < 8 && ((d->max_len + ctas - 1) / ctas > cap || (l.units * ctas * 2 <= 2 * PAGED_SMS && d->max_len > ctas * 128))) ctas *= 2;
-    l.fused = d->max_len <= ctas * cap && l.units * ctas <= 2 * PAGED_SMS;
+    l.fused = d->max_len <= ctas * cap && (ctas == 1 || l.units * ctas <= 2 * PAGED_SMS);
     if (l.fused) {
         l.ctas = ctas;
         l.span = ((d->max_len + ctas - 1) / ctas + 31) / 32 * 32;
