@@ -23,7 +23,7 @@ struct PagedArgs {
     int* status;
     int group, blocks_per_head;   // query heads of a key head; units that they make
     int64_t page_bytes, token_bytes;      // distances of pages and tokens in the caches
-    uint32_t div_mul, div_shift;          // j / page_size = umulhi(j, div_mul) >> div_shift for every token number j (page_size > 1)
+    NmDivisor by_page;                    // by page_size
     int span;                     // fused: tokens that a block's shared memory holds; split: tokens that a block has at least
     int64_t row;                  // split: scores of one head in the workspace
     float *scores, *maxima;       // split: [B][heads][row]; [B][heads], of units that one block has
@@ -89,7 +89,7 @@ template <int TILE> struct PagedCursor {
     }
     __device__ __forceinline__ void look()
     {
-        const int j = tok.first + token, entry = a.d.page_size == 1 ? j : (int)(__umulhi((uint32_t)j, a.div_mul) >> a.div_shift);
+        const int j = tok.first + token, entry = a.by_page(j);
         place = j - entry * a.d.page_size;
         page = token < tok.count ? tok.table[entry] : -1;
     }
@@ -1142,13 +1142,7 @@ nm_status nm_launch_attention_paged(nm_ctx* ctx, const nm_attn_paged_desc* d, vo
     const int es = (int)nm_dtype_size(d->dtype);
     a.page_bytes = d->stride_page * es;
     a.token_bytes = d->stride_token * es;
-    a.div_mul = a.div_shift = 0;
-    if (d->page_size > 1) {   // 2^(31 + l) / page_size rounded up, l = ceil(log2(page_size)): right for all numbers of 31 bits
-        int l = 1;
-        while (((int64_t)1 << l) < d->page_size) ++l;
-        a.div_mul = (uint32_t)(((uint64_t)1 << (31 + l)) / (uint32_t)d->page_size + 1);
-        a.div_shift = (uint32_t)(l - 1);
-    }
+    a.by_page = NmDivisor::of(d->page_size);
     a.row = l.row;
     uint8_t* ws = (uint8_t*)workspace;
     a.scores = (float*)(ws + l.scores);

@@ -69,6 +69,7 @@ nm_status nm_qk_norm_rope_pwl(nm_ctx* ctx, const nm_qk_rope_desc* d, void* strea
     }
     if (d->T == 0 || (d->heads == 0 && d->kv_heads == 0)) return NM_OK;
     const int64_t row = ((int64_t)d->heads + 2 * (int64_t)d->kv_heads) * d->d;
+    if (row > INT32_MAX) return NM_ERR_SHAPE;
     if (!d->qkv || (d->heads > 0 && !d->q_out)) return NM_ERR_INVALID_ARG;
     if (d->ld_qkv < row || (d->heads > 0 && d->ld_q < (int64_t)d->heads * d->d)) return NM_ERR_SHAPE;
     if (d->k_out && d->ld_k < (int64_t)d->kv_heads * d->d) return NM_ERR_SHAPE;

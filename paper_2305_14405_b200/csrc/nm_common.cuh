@@ -847,3 +847,21 @@ struct NmLaunchConfig {
         }
     }
 };
+
+// Division of whole numbers of 31 bits by one that a launch fixes: a / d = umulhi(a, mul) >> shift with mul = 2^(31 + l) / d rounded up,
+// l = ceil(log2(d)); d = 1 is a case of its own (mul = 0).
+struct NmDivisor {
+    uint32_t mul, shift;
+    static NmDivisor of(int d)
+    {
+        NmDivisor r = {0, 0};
+        if (d > 1) {
+            int l = 1;
+            while (((int64_t)1 << l) < d) ++l;
+            r.mul = (uint32_t)(((uint64_t)1 << (31 + l)) / (uint32_t)d + 1);
+            r.shift = (uint32_t)(l - 1);
+        }
+        return r;
+    }
+    __device__ __forceinline__ int operator()(int a) const { return mul ? (int)(__umulhi((uint32_t)a, mul) >> shift) : a; }
+};
