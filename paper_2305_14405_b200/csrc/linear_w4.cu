@@ -9,6 +9,8 @@
 //
 // Every warp streams its own weights through a ring of asynchronous copies (256 codes of 16 or 32 rows a stage, so 128 bytes a row):
 // no barrier in the loop.  Activations come through L1, shared by the warps of a block that work on the same k.
+#include <type_traits>
+
 #include "nm_common.cuh"
 
 namespace {
@@ -18,7 +20,7 @@ constexpr int W4_WARPS = 8, W4_THREADS = W4_WARPS * 32, W4_BLOCK_K = 256, W4_TIL
 struct W4Args {
     nm_linear_w4_desc d;
     const NmTable* tab;
-    int row_warps, k_blocks, row_blocks;
+    int row_warps, k_blocks, k_groups, row_blocks;
 };
 
 template <typename T> struct W4Type {
@@ -43,77 +45,83 @@ __device__ __forceinline__ void w4_mma(float* c, const uint32_t* a, uint32_t b0,
         : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
 
-// Codes i and i + 4 of a word as a pair of whole numbers -8..7.
-__device__ __forceinline__ uint32_t w4_pair(uint32_t w, int i, __nv_bfloat16)
+// The eight codes of a word as pairs (i, i + 4) of whole numbers -8..7.
+__device__ __forceinline__ uint32_t w4_sub(uint32_t v, float c, __nv_bfloat16)
 {
-    const uint32_t v = ((w >> (4 * i)) & 0x000f000fu) | 0x43004300u;   // 128 + c
-    const __nv_bfloat162 r = __hsub2(*reinterpret_cast<const __nv_bfloat162*>(&v), __floats2bfloat162_rn(136.f, 136.f));
+    const __nv_bfloat162 r = __hsub2(*reinterpret_cast<const __nv_bfloat162*>(&v), __floats2bfloat162_rn(c, c));
     return *reinterpret_cast<const uint32_t*>(&r);
 }
-__device__ __forceinline__ uint32_t w4_pair(uint32_t w, int i, __half)
+__device__ __forceinline__ void w4_pairs(uint32_t w, uint32_t* p, __nv_bfloat16)
 {
-    const uint32_t v = ((w >> (4 * i)) & 0x000f000fu) | 0x64006400u;   // 1024 + c
-    const __half2 r = __hsub2(*reinterpret_cast<const __half2*>(&v), __floats2half2_rn(1032.f, 1032.f));
-    return *reinterpret_cast<const uint32_t*>(&r);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) p[i] = w4_sub(((w >> (4 * i)) & 0x000f000fu) | 0x43004300u, 136.f, __nv_bfloat16());   // 128 + c
+}
+__device__ __forceinline__ void w4_pairs(uint32_t w, uint32_t* p, __half)
+{
+    // 1024 + c from the low half of a byte, 1024 + 16 c from the high one, which needs no shift: times 1/16, all of it exact
+    const uint32_t h = w >> 8, magic = 0x64006400u;
+    const uint32_t v[4] = {(w & 0x000f000fu) | magic, (w & 0x00f000f0u) | magic, (h & 0x000f000fu) | magic, (h & 0x00f000f0u) | magic};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const __half2 x = *reinterpret_cast<const __half2*>(&v[i]);
+        const __half2 r = i & 1 ? __hfma2(x, __floats2half2_rn(0.0625f, 0.0625f), __floats2half2_rn(-72.f, -72.f)) : __hsub2(x, __floats2half2_rn(1032.f, 1032.f));
+        p[i] = *reinterpret_cast<const uint32_t*>(&r);
+    }
 }
 
-// Eight activations of one token as pairs (i, i + 4), for every term.
-template <typename T> struct W4Acts {
-    static constexpr int TERMS = W4Type<T>::TERMS;
-    uint32_t p[TERMS][4];
+// Eight activations of one token as they lie in memory, and as pairs (i, i + 4) for every term.
+template <typename T> struct W4Raw {
+    static constexpr int VECS = sizeof(T) / 2, TERMS = W4Type<T>::TERMS;
+    uint4 v[VECS];
+    __device__ __forceinline__ void load(const T* x)
+    {
+#pragma unroll
+        for (int i = 0; i < VECS; ++i) v[i] = __ldg(reinterpret_cast<const uint4*>(x) + i);
+    }
     __device__ __forceinline__ void zero()
     {
 #pragma unroll
-        for (int s = 0; s < TERMS; ++s)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) p[s][i] = 0;
+        for (int i = 0; i < VECS; ++i) v[i] = make_uint4(0, 0, 0, 0);
     }
-    __device__ __forceinline__ void load(const T* x)
+    __device__ __forceinline__ void pairs(uint32_t (&p)[TERMS][4]) const
     {
         if constexpr (TERMS == 1) {
-            const uint4 v = __ldg(reinterpret_cast<const uint4*>(x));
-            p[0][0] = __byte_perm(v.x, v.z, 0x5410);
-            p[0][1] = __byte_perm(v.x, v.z, 0x7632);
-            p[0][2] = __byte_perm(v.y, v.w, 0x5410);
-            p[0][3] = __byte_perm(v.y, v.w, 0x7632);
+            p[0][0] = __byte_perm(v[0].x, v[0].z, 0x5410);
+            p[0][1] = __byte_perm(v[0].x, v[0].z, 0x7632);
+            p[0][2] = __byte_perm(v[0].y, v[0].w, 0x5410);
+            p[0][3] = __byte_perm(v[0].y, v[0].w, 0x7632);
         } else {
-            const float4 lo = __ldg(reinterpret_cast<const float4*>(x)), hi = __ldg(reinterpret_cast<const float4*>(x) + 1);
-            const float a[4] = {lo.x, lo.y, lo.z, lo.w}, b[4] = {hi.x, hi.y, hi.z, hi.w};
+            const uint32_t a[4] = {v[0].x, v[0].y, v[0].z, v[0].w}, b[4] = {v[VECS - 1].x, v[VECS - 1].y, v[VECS - 1].z, v[VECS - 1].w};
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 uint32_t ta[3], tb[3];
                 split(a[i], ta);
                 split(b[i], tb);
 #pragma unroll
-                for (int s = 0; s < 3; ++s) p[s][i] = __byte_perm(ta[s], tb[s], 0x7632);
+                for (int s = 0; s < TERMS; ++s) p[s][i] = __byte_perm(ta[s], tb[s], 0x7632);
             }
         }
     }
     // x as three bf16 numbers in the upper halves: the first two cut off (so none of them overflows), the rest has 8 bits left.
     // What is not finite stays in the first term alone (an infinity's rest would be NaN).
-    static __device__ __forceinline__ void split(float x, uint32_t* t)
+    static __device__ __forceinline__ void split(uint32_t bits, uint32_t* t)
     {
-        const uint32_t bits = __float_as_uint(x);
-        if ((bits & 0x7f800000u) == 0x7f800000u) {
-            t[0] = (bits & 0x007fffffu) ? 0x7fc00000u : bits;
-            t[1] = t[2] = 0;
-            return;
-        }
-        t[0] = bits & 0xffff0000u;
-        const float r = x - __uint_as_float(t[0]);
+        const bool finite = (bits & 0x7f800000u) != 0x7f800000u;
+        t[0] = finite ? bits & 0xffff0000u : (bits & 0x007fffffu) ? 0x7fc00000u : bits;
+        const float r = finite ? __uint_as_float(bits) - __uint_as_float(t[0]) : 0.f;
         t[1] = __float_as_uint(r) & 0xffff0000u;
         t[2] = __float_as_uint(r - __uint_as_float(t[1])) & 0xffff0000u;
     }
 };
 
-template <int BYTES> __device__ __forceinline__ void w4_copy(uint32_t dst, const void* src, bool valid)
+__device__ __forceinline__ void w4_copy(uint32_t dst, const void* src, bool valid)
 {
-    asm volatile("cp.async.cg.shared.global [%0], [%1], %2, %3;" ::"r"(dst), "l"(src), "n"(BYTES), "r"(valid ? BYTES : 0) : "memory");
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(valid ? 16 : 0) : "memory");
 }
 
 // NT tiles of 8 tokens, RW tiles of 16 weight rows per warp.  row_warps warps of a block lie along the rows, the others and the
 // CTAs of a cluster split k, block by block in turn; their sums are added in that order at the end.
-template <typename T, int NT, int RW, int STAGES>
+template <typename T, int NT, int RW, int STAGES, int GS>
 __global__ void __launch_bounds__(W4_THREADS, 2) linear_w4_kernel(const W4Args a)
 {
     using Mma = typename W4Type<T>::Mma;
@@ -126,8 +134,8 @@ __global__ void __launch_bounds__(W4_THREADS, 2) linear_w4_kernel(const W4Args a
     uint32_t ctas;
     asm("mov.u32 %0, %%cluster_nctarank;" : "=r"(ctas));
     const uint32_t rank = nm_cluster_ctarank();
-    const int64_t unit = blockIdx.x / ctas;
-    const int64_t m0 = unit / a.row_blocks * (NT * 8), block_row = unit % a.row_blocks * (16 * RW * a.row_warps);
+    const uint32_t unit = blockIdx.x / ctas;
+    const int64_t m0 = (int64_t)(unit / a.row_blocks) * (NT * 8), block_row = (int64_t)(unit % a.row_blocks) * (16 * RW * a.row_warps);
     const int64_t n0 = block_row + row_warp * (16 * RW);
     const int step = k_warps * (int)ctas, first = (int)rank * k_warps + k_warp;
     unsigned char* ring = w4_smem + warp * RING;
@@ -135,33 +143,65 @@ __global__ void __launch_bounds__(W4_THREADS, 2) linear_w4_kernel(const W4Args a
     nm_grid_launch_dependents();
     nm_grid_dependency_wait();
 
+    // 16-byte piece c of a row lies at place c ^ (row & 7): word reads hit all banks.  Rows behind the last one are read as its copy, their
+    // sums are not stored.
     const int copy_row = lane >> 3, copy_chunk = lane & 7;
+    const uint8_t* from[RW * 4];
+    uint32_t to[RW * 4];
+#pragma unroll
+    for (int r = 0; r < RW * 4; ++r) {
+        const int row = r * 4 + copy_row;
+        from[r] = d.codes + (n0 + row < d.N ? n0 + row : d.N - 1) * d.ld_codes + copy_chunk * 16;
+        to[r] = ring_at + row * 128 + ((copy_chunk ^ (row & 7)) << 4);
+    }
     auto fetch = [&](int b, int stage) {
         if (b < a.k_blocks) {
-            const int64_t at = (int64_t)b * (W4_BLOCK_K / 2) + copy_chunk * 16;
-            const bool in_k = at * 2 < d.K;
+            const int64_t at = (int64_t)b * (W4_BLOCK_K / 2);
+            const bool valid = b + 1 < a.k_blocks || (at + copy_chunk * 16) * 2 < d.K;   // the last block may be short
 #pragma unroll
-            for (int r = 0; r < RW * 4; ++r) {
-                const int row = r * 4 + copy_row;   // 16-byte piece c of a row lies at place c ^ (row & 7): word reads hit all banks
-                const bool valid = in_k && n0 + row < d.N;
-                w4_copy<16>(ring_at + stage * (RW * W4_TILE) + row * 128 + ((copy_chunk ^ (row & 7)) << 4),
-                            valid ? d.codes + (n0 + row) * d.ld_codes + at : d.codes, valid);
-            }
+            for (int r = 0; r < RW * 4; ++r) w4_copy(to[r] + stage * (RW * W4_TILE), valid ? from[r] + at : d.codes, valid);
         }
         asm volatile("cp.async.commit_group;" ::: "memory");
     };
-    float sum[RW][NT][4], part[RW][NT][4];
+    float sum[RW][NT][4];
 #pragma unroll
     for (int r = 0; r < RW; ++r)
 #pragma unroll
         for (int n = 0; n < NT; ++n)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) sum[r][n][i] = part[r][n][i] = 0.f;
+            for (int i = 0; i < 4; ++i) sum[r][n][i] = 0.f;
 #pragma unroll
     for (int s = 0; s < STAGES - 1; ++s) fetch(first + s * step, s);
 
-    const int groups = W4_BLOCK_K / d.group, flush = d.group / 32 - 1;   // groups of a block; a group ends where (j & flush) == flush
-    const T* scales = (const T*)d.scales;
+    constexpr int groups = 8 / GS;   // of a block
+    // Scales of groups t and t + 4 of a block, of rows g and g + 8; handed round among four lanes below.  The next block's are on their
+    // way while one is worked on: they lie a row apart, and so far apart that each load waits for memory.
+    const T* scales[RW][2];
+#pragma unroll
+    for (int r = 0; r < RW; ++r)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const int64_t row = n0 + r * 16 + h * 8 + g;
+            scales[r][h] = (const T*)d.scales + (row < d.N ? row : d.N - 1) * d.ld_scales + t;
+        }
+    T sc[RW][2][2], sc_next[RW][2][2];
+    auto look = [&](int b) {
+        if (b >= a.k_blocks) return;
+        const int at = b * groups, left = a.k_groups - at;   // groups of a row fit 31 bits
+#pragma unroll
+        for (int q = 0; q < (GS == 1 ? 2 : 1); ++q)
+            if (t + 4 * q < groups && t + 4 * q < left) {
+#pragma unroll
+                for (int r = 0; r < RW; ++r)
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) sc_next[r][h][q] = scales[r][h][at + 4 * q];
+            }
+    };
+#pragma unroll
+    for (int r = 0; r < RW; ++r)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) sc_next[r][h][0] = sc_next[r][h][1] = NmType<T>::from_f(0.f);
+    look(first);
     const T* acts[NT];
     bool token[NT];
 #pragma unroll
@@ -169,65 +209,86 @@ __global__ void __launch_bounds__(W4_THREADS, 2) linear_w4_kernel(const W4Args a
         token[n] = m0 + n * 8 + g < d.M;
         acts[n] = (const T*)d.A + (token[n] ? (m0 + n * 8 + g) * d.lda : 0) + t * 8;
     }
+    constexpr int CJ = 4 / (NT * W4Raw<T>::VECS) > 1 ? 4 / (NT * W4Raw<T>::VECS) : 1;   // steps of 32 k whose activations are loaded ahead
     int stage = 0;
     for (int b = first; b < a.k_blocks; b += step) {
         fetch(b + (STAGES - 1) * step, stage == 0 ? STAGES - 1 : stage - 1);
-        // scales of groups t and t + 4 of the block, of rows g and g + 8; handed round among four lanes below
-        float sc[RW][2][2];
 #pragma unroll
         for (int r = 0; r < RW; ++r)
 #pragma unroll
             for (int h = 0; h < 2; ++h)
 #pragma unroll
-                for (int q = 0; q < 2; ++q) {
-                    const int64_t row = n0 + r * 16 + h * 8 + g;
-                    const int gi = t + 4 * q;
-                    const int64_t at = (int64_t)b * groups + gi;
-                    sc[r][h][q] = gi < groups && at * d.group < d.K && row < d.N ? NmType<T>::to_f(scales[row * d.ld_scales + at]) : 0.f;
-                }
-        asm volatile("cp.async.wait_group %0;" ::"n"(STAGES - 1) : "memory");
-        __syncwarp();
-        const unsigned char* tile = ring + stage * (RW * W4_TILE);
+                for (int q = 0; q < 2; ++q) sc[r][h][q] = sc_next[r][h][q];
+        look(b + step);
         const int64_t k0 = (int64_t)b * W4_BLOCK_K;
+        const int steps = d.K - k0 >= W4_BLOCK_K ? 8 : (int)(d.K - k0) / 32;   // K is a multiple of 32
+        const unsigned char* tile = ring + stage * (RW * W4_TILE);
+        // FULL: all eight steps, with no branch between them
+        auto block = [&](auto full) {
+            constexpr bool FULL = decltype(full)::value;
+            W4Raw<T> ahead[2][CJ][NT];
+            auto load = [&](int j0, W4Raw<T> (&x)[CJ][NT]) {
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            if (k0 + j * 32 < d.K) {   // the same for the whole warp: K is a multiple of 32
-                W4Acts<T> x[NT];
+                for (int j = 0; j < CJ; ++j)
 #pragma unroll
-                for (int n = 0; n < NT; ++n) {
-                    x[n].zero();
-                    if (token[n]) x[n].load(acts[n] + k0 + j * 32);
-                }
-#pragma unroll
-                for (int r = 0; r < RW; ++r) {
-                    const uint32_t w0 = *reinterpret_cast<const uint32_t*>(tile + (r * 16 + g) * 128 + ((j ^ g) << 4) + t * 4);
-                    const uint32_t w1 = *reinterpret_cast<const uint32_t*>(tile + (r * 16 + g + 8) * 128 + ((j ^ g) << 4) + t * 4);
-#pragma unroll
-                    for (int p = 0; p < 4; p += 2) {
-                        const uint32_t f[4] = {w4_pair(w0, p, Mma()), w4_pair(w1, p, Mma()), w4_pair(w0, p + 1, Mma()), w4_pair(w1, p + 1, Mma())};
-#pragma unroll
-                        for (int n = 0; n < NT; ++n)
-#pragma unroll
-                            for (int s = 0; s < TERMS; ++s) w4_mma(part[r][n], f, x[n].p[s][p], x[n].p[s][p + 1], Mma());
+                    for (int n = 0; n < NT; ++n) {
+                        x[j][n].zero();
+                        if (token[n] && (FULL || j0 + j < steps)) x[j][n].load(acts[n] + k0 + (j0 + j) * 32);
                     }
-                }
-                if ((j & flush) == flush) {
-                    const int gi = j / (flush + 1), from = (lane & 28) | (gi & 3);
+            };
+            load(0, ahead[0]);
+            asm volatile("cp.async.wait_group %0;" ::"n"(STAGES - 1) : "memory");
+            __syncwarp();
+            float part[RW][NT][4];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                if (j % CJ == 0 && j + CJ < 8) load(j + CJ, ahead[(j / CJ + 1) & 1]);
+                if (FULL || j < steps) {   // the same for the whole warp
+                    uint32_t x[NT][TERMS][4];
+#pragma unroll
+                    for (int n = 0; n < NT; ++n) ahead[(j / CJ) & 1][j % CJ][n].pairs(x[n]);
+                    if (j % GS == 0) {
+#pragma unroll
+                        for (int r = 0; r < RW; ++r)
+#pragma unroll
+                            for (int n = 0; n < NT; ++n)
+#pragma unroll
+                                for (int i = 0; i < 4; ++i) part[r][n][i] = 0.f;
+                    }
 #pragma unroll
                     for (int r = 0; r < RW; ++r) {
-                        const float s0 = __shfl_sync(0xffffffffu, gi < 4 ? sc[r][0][0] : sc[r][0][1], from);
-                        const float s1 = __shfl_sync(0xffffffffu, gi < 4 ? sc[r][1][0] : sc[r][1][1], from);
+                        const uint32_t w0 = *reinterpret_cast<const uint32_t*>(tile + (r * 16 + g) * 128 + ((j ^ g) << 4) + t * 4);
+                        const uint32_t w1 = *reinterpret_cast<const uint32_t*>(tile + (r * 16 + g + 8) * 128 + ((j ^ g) << 4) + t * 4);
+                        uint32_t lo[4], hi[4];
+                        w4_pairs(w0, lo, Mma());
+                        w4_pairs(w1, hi, Mma());
 #pragma unroll
-                        for (int n = 0; n < NT; ++n)
+                        for (int p = 0; p < 4; p += 2) {
+                            const uint32_t f[4] = {lo[p], hi[p], lo[p + 1], hi[p + 1]};
 #pragma unroll
-                            for (int i = 0; i < 4; ++i) {
-                                sum[r][n][i] = __fmaf_rn(i < 2 ? s0 : s1, part[r][n][i], sum[r][n][i]);
-                                part[r][n][i] = 0.f;
-                            }
+                            for (int n = 0; n < NT; ++n)
+#pragma unroll
+                                for (int s = 0; s < TERMS; ++s) w4_mma(part[r][n], f, x[n][s][p], x[n][s][p + 1], Mma());
+                        }
+                    }
+                    if (j % GS == GS - 1) {   // a group ends
+                        constexpr int Q = GS == 1 ? 4 : 8;
+                        const int gi = j / GS, from_lane = (lane & 28) | (gi & 3);
+#pragma unroll
+                        for (int r = 0; r < RW; ++r) {
+                            const float s0 = __shfl_sync(0xffffffffu, NmType<T>::to_f(sc[r][0][gi / 4 % (8 / Q)]), from_lane);
+                            const float s1 = __shfl_sync(0xffffffffu, NmType<T>::to_f(sc[r][1][gi / 4 % (8 / Q)]), from_lane);
+#pragma unroll
+                            for (int n = 0; n < NT; ++n)
+#pragma unroll
+                                for (int i = 0; i < 4; ++i) sum[r][n][i] = __fmaf_rn(i < 2 ? s0 : s1, part[r][n][i], sum[r][n][i]);
+                        }
                     }
                 }
             }
-        }
+        };
+        if (steps == 8) block(std::true_type());
+        else block(std::false_type());
         __syncwarp();   // the stage may be filled again
         stage = stage == STAGES - 1 ? 0 : stage + 1;
     }
@@ -270,13 +331,14 @@ __global__ void __launch_bounds__(W4_THREADS, 2) linear_w4_kernel(const W4Args a
     if (ctas > 1) nm_cluster_sync();   // no CTA leaves while another reads its shared memory
 }
 
-template <typename T, int NT, int RW>
+template <typename T, int NT, int RW, int GS>
 nm_status launch(nm_ctx* ctx, const nm_linear_w4_desc* d, cudaStream_t st)
 {
     constexpr int STAGES = RW == 1 ? 4 : 3, SMEM = W4_WARPS * STAGES * RW * W4_TILE;
     W4Args a;
     a.d = *d;
     a.tab = d->slot == NM_SLOT_NONE ? nullptr : ctx->d_tables + d->slot;
+    a.k_groups = (int)(d->K / d->group);
     a.k_blocks = (int)((d->K + W4_BLOCK_K - 1) / W4_BLOCK_K);
     const int64_t token_blocks = (d->M + NT * 8 - 1) / (NT * 8), row_tiles = (d->N + 16 * RW - 1) / (16 * RW);
     // A block reads its tokens' activations once for all its rows: as many rows as keep those bytes below the weights' (4 M / rows).
@@ -290,20 +352,25 @@ nm_status launch(nm_ctx* ctx, const nm_linear_w4_desc* d, cudaStream_t st)
     int ctas = 1;   // of a cluster: they split k further while there is room
     while (ctas < 8 && units * ctas * 2 <= slots && a.k_blocks >= 2 * ctas * (W4_WARPS / rw)) ctas *= 2;
     if (units * ctas > INT32_MAX) return NM_ERR_SHAPE;
-    auto kernel = linear_w4_kernel<T, NT, RW, STAGES>;
+    auto kernel = linear_w4_kernel<T, NT, RW, STAGES, GS>;
     if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM) != cudaSuccess) return NM_ERR_CUDA;
     NmLaunchScope scope(ctx, NM_KERNEL_LINEAR_W4, 0.5 * d->N * d->K, st);
     NmLaunchConfig lc(ctx, dim3((unsigned)(units * ctas)), W4_THREADS, SMEM, st, ctas);
     return cudaLaunchKernelEx(&lc.cfg, kernel, a) == cudaSuccess ? NM_OK : NM_ERR_CUDA;
 }
 
+template <typename T, int GS>
+nm_status by_tokens(nm_ctx* ctx, const nm_linear_w4_desc* d, cudaStream_t st)
+{
+    // one tile of weight rows per warp where the activations are few beside them, two otherwise (each then serves two products)
+    if (d->M <= 8) return launch<T, 1, sizeof(T) == 4 ? 2 : 1, GS>(ctx, d, st);
+    if (d->M <= 16) return launch<T, 2, 2, GS>(ctx, d, st);
+    return launch<T, 4, 2, GS>(ctx, d, st);
+}
 template <typename T>
 nm_status dispatch(nm_ctx* ctx, const nm_linear_w4_desc* d, cudaStream_t st)
 {
-    // one tile of weight rows per warp where the activations are few beside them, two otherwise (each then serves two products)
-    if (d->M <= 8) return launch<T, 1, sizeof(T) == 4 ? 2 : 1>(ctx, d, st);
-    if (d->M <= 16) return launch<T, 2, 2>(ctx, d, st);
-    return launch<T, 4, 2>(ctx, d, st);
+    return d->group == 32 ? by_tokens<T, 1>(ctx, d, st) : d->group == 64 ? by_tokens<T, 2>(ctx, d, st) : by_tokens<T, 4>(ctx, d, st);
 }
 
 }  // namespace
