@@ -121,11 +121,15 @@ __device__ __forceinline__ void w4_copy(uint32_t dst, const void* src, bool vali
 
 // NT tiles of 8 tokens, RW tiles of 16 weight rows per warp.  row_warps warps of a block lie along the rows, the others and the
 // CTAs of a cluster split k, block by block in turn; their sums are added in that order at the end.
+// Activations of up to 8 tokens are loaded by each warp for itself, through L1.  More tokens are shared (STAGED): all warps lay the pairs
+// of a slice of k out in shared memory as the products take them, once for all of the block's rows, a slice ahead of their use.
 template <typename T, int NT, int RW, int STAGES, int GS>
 __global__ void __launch_bounds__(W4_THREADS, 2) linear_w4_kernel(const W4Args a)
 {
     using Mma = typename W4Type<T>::Mma;
+    constexpr bool STAGED = NT > 1;
     constexpr int TERMS = W4Type<T>::TERMS, RING = STAGES * RW * W4_TILE, PITCH = 16 * RW + 4;
+    constexpr int FRAG = NT * TERMS * 512;   // STAGED: pairs of 32 k
     static_assert(NT * 8 * PITCH * 4 <= RING, "a warp's sums fit its ring");
     extern __shared__ __align__(128) unsigned char w4_smem[];
     const nm_linear_w4_desc& d = a.d;
@@ -146,20 +150,18 @@ __global__ void __launch_bounds__(W4_THREADS, 2) linear_w4_kernel(const W4Args a
     // 16-byte piece c of a row lies at place c ^ (row & 7): word reads hit all banks.  Rows behind the last one are read as its copy, their
     // sums are not stored.
     const int copy_row = lane >> 3, copy_chunk = lane & 7;
-    const uint8_t* from[RW * 4];
-    uint32_t to[RW * 4];
+    const uint8_t* from = d.codes + (n0 + copy_row < d.N ? n0 + copy_row : d.N - 1) * d.ld_codes + copy_chunk * 16;
+    int down[RW * 4];   // rows from there to row r * 4 + copy_row
 #pragma unroll
-    for (int r = 0; r < RW * 4; ++r) {
-        const int row = r * 4 + copy_row;
-        from[r] = d.codes + (n0 + row < d.N ? n0 + row : d.N - 1) * d.ld_codes + copy_chunk * 16;
-        to[r] = ring_at + row * 128 + ((copy_chunk ^ (row & 7)) << 4);
-    }
+    for (int r = 0; r < RW * 4; ++r) down[r] = n0 + copy_row >= d.N ? 0 : n0 + copy_row + r * 4 < d.N ? r * 4 : (int)(d.N - 1 - n0 - copy_row);
+    const uint32_t to[2] = {ring_at + copy_row * 128 + ((copy_chunk ^ copy_row) << 4), ring_at + (copy_row + 4) * 128 + ((copy_chunk ^ (copy_row + 4)) << 4)};
     auto fetch = [&](int b, int stage) {
         if (b < a.k_blocks) {
             const int64_t at = (int64_t)b * (W4_BLOCK_K / 2);
             const bool valid = b + 1 < a.k_blocks || (at + copy_chunk * 16) * 2 < d.K;   // the last block may be short
 #pragma unroll
-            for (int r = 0; r < RW * 4; ++r) w4_copy(to[r] + stage * (RW * W4_TILE), valid ? from[r] + at : d.codes, valid);
+            for (int r = 0; r < RW * 4; ++r)
+                w4_copy(to[r & 1] + (r >> 1) * 1024 + stage * (RW * W4_TILE), valid ? from + down[r] * d.ld_codes + at : d.codes, valid);
         }
         asm volatile("cp.async.commit_group;" ::: "memory");
     };
@@ -209,143 +211,221 @@ __global__ void __launch_bounds__(W4_THREADS, 2) linear_w4_kernel(const W4Args a
         token[n] = m0 + n * 8 + g < d.M;
         acts[n] = (const T*)d.A + (token[n] ? (m0 + n * 8 + g) * d.lda : 0) + t * 8;
     }
-    constexpr int CJ = 4 / (NT * W4Raw<T>::VECS) > 1 ? 4 / (NT * W4Raw<T>::VECS) : 1;   // steps of 32 k whose activations are loaded ahead
-    int stage = 0;
-    for (int b = first; b < a.k_blocks; b += step) {
-        fetch(b + (STAGES - 1) * step, stage == 0 ? STAGES - 1 : stage - 1);
+    // STAGED: warp w lays out step w of each of the slice's k_warps blocks (at most 4 / NT)
+    constexpr int SLOTS = STAGED ? 4 / NT : 1;
+    W4Raw<T> mine[SLOTS][NT];
+    unsigned char* shared_acts = w4_smem + W4_WARPS * RING;
+    auto gather = [&](int slice) {
 #pragma unroll
-        for (int r = 0; r < RW; ++r)
+        for (int k = 0; k < SLOTS; ++k)
 #pragma unroll
-            for (int h = 0; h < 2; ++h)
+            for (int n = 0; n < NT; ++n) {
+                mine[k][n].zero();
+                const int64_t at = ((int64_t)slice * k_warps + k) * W4_BLOCK_K + warp * 32;
+                if (k < k_warps && token[n] && at < d.K) mine[k][n].load(acts[n] + at);
+            }
+    };
+    auto lay_out = [&](int half) {
 #pragma unroll
-                for (int q = 0; q < 2; ++q) sc[r][h][q] = sc_next[r][h][q];
-        look(b + step);
-        const int64_t k0 = (int64_t)b * W4_BLOCK_K;
-        const int steps = d.K - k0 >= W4_BLOCK_K ? 8 : (int)(d.K - k0) / 32;   // K is a multiple of 32
-        const unsigned char* tile = ring + stage * (RW * W4_TILE);
-        // FULL: all eight steps, with no branch between them
-        auto block = [&](auto full) {
-            constexpr bool FULL = decltype(full)::value;
-            W4Raw<T> ahead[2][CJ][NT];
-            auto load = [&](int j0, W4Raw<T> (&x)[CJ][NT]) {
+        for (int k = 0; k < SLOTS; ++k)
+            if (k < k_warps) {
 #pragma unroll
-                for (int j = 0; j < CJ; ++j)
+                for (int n = 0; n < NT; ++n) {
+                    uint32_t x[TERMS][4];
+                    mine[k][n].pairs(x);
 #pragma unroll
-                    for (int n = 0; n < NT; ++n) {
-                        x[j][n].zero();
-                        if (token[n] && (FULL || j0 + j < steps)) x[j][n].load(acts[n] + k0 + (j0 + j) * 32);
-                    }
-            };
-            load(0, ahead[0]);
-            asm volatile("cp.async.wait_group %0;" ::"n"(STAGES - 1) : "memory");
-            __syncwarp();
-            float part[RW][NT][4];
+                    for (int s = 0; s < TERMS; ++s)
+                        reinterpret_cast<uint4*>(shared_acts + ((half * k_warps + k) * 8 + warp) * FRAG + (n * TERMS + s) * 512)[lane] =
+                            make_uint4(x[s][0], x[s][1], x[s][2], x[s][3]);
+                }
+            }
+    };
+    constexpr int CJ = STAGED ? 1 : 4 / W4Raw<T>::VECS;   // steps of 32 k whose activations are loaded ahead
+    const int slices = (a.k_blocks + k_warps - 1) / k_warps;
+    if constexpr (STAGED) {
+        if ((int)rank < slices) {
+            gather(rank);
+            lay_out(0);
+        }
+        __syncthreads();
+    }
+    int stage = 0, half = 0;
+    for (int slice = rank; slice < slices; slice += ctas) {   // the same for all warps
+        const int b = slice * k_warps + k_warp;
+        if constexpr (STAGED) {
+            if (slice + (int)ctas < slices) gather(slice + ctas);
+        }
+        if (b < a.k_blocks) {
+            fetch(b + (STAGES - 1) * step, stage == 0 ? STAGES - 1 : stage - 1);
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                if (j % CJ == 0 && j + CJ < 8) load(j + CJ, ahead[(j / CJ + 1) & 1]);
-                if (FULL || j < steps) {   // the same for the whole warp
-                    uint32_t x[NT][TERMS][4];
+            for (int r = 0; r < RW; ++r)
 #pragma unroll
-                    for (int n = 0; n < NT; ++n) ahead[(j / CJ) & 1][j % CJ][n].pairs(x[n]);
-                    if (j % GS == 0) {
+                for (int h = 0; h < 2; ++h)
 #pragma unroll
-                        for (int r = 0; r < RW; ++r)
+                    for (int q = 0; q < 2; ++q) sc[r][h][q] = sc_next[r][h][q];
+            look(b + step);
+            const int64_t k0 = (int64_t)b * W4_BLOCK_K;
+            const int steps = d.K - k0 >= W4_BLOCK_K ? 8 : (int)(d.K - k0) / 32;   // K is a multiple of 32
+            const unsigned char* tile = ring + stage * (RW * W4_TILE);
+            const unsigned char* frags = shared_acts + (half * k_warps + k_warp) * 8 * FRAG;
+            // FULL: all eight steps, with no branch between them
+            auto block = [&](auto full) {
+                constexpr bool FULL = decltype(full)::value;
+                W4Raw<T> ahead[2][CJ];
+                auto load = [&](int j0, W4Raw<T> (&x)[CJ]) {
+                    if constexpr (!STAGED) {
 #pragma unroll
-                            for (int n = 0; n < NT; ++n)
-#pragma unroll
-                                for (int i = 0; i < 4; ++i) part[r][n][i] = 0.f;
-                    }
-#pragma unroll
-                    for (int r = 0; r < RW; ++r) {
-                        const uint32_t w0 = *reinterpret_cast<const uint32_t*>(tile + (r * 16 + g) * 128 + ((j ^ g) << 4) + t * 4);
-                        const uint32_t w1 = *reinterpret_cast<const uint32_t*>(tile + (r * 16 + g + 8) * 128 + ((j ^ g) << 4) + t * 4);
-                        uint32_t lo[4], hi[4];
-                        w4_pairs(w0, lo, Mma());
-                        w4_pairs(w1, hi, Mma());
-#pragma unroll
-                        for (int p = 0; p < 4; p += 2) {
-                            const uint32_t f[4] = {lo[p], hi[p], lo[p + 1], hi[p + 1]};
-#pragma unroll
-                            for (int n = 0; n < NT; ++n)
-#pragma unroll
-                                for (int s = 0; s < TERMS; ++s) w4_mma(part[r][n], f, x[n][s][p], x[n][s][p + 1], Mma());
+                        for (int j = 0; j < CJ; ++j) {
+                            x[j].zero();
+                            if (token[0] && (FULL || j0 + j < steps)) x[j].load(acts[0] + k0 + (j0 + j) * 32);
                         }
                     }
-                    if (j % GS == GS - 1) {   // a group ends
-                        constexpr int Q = GS == 1 ? 4 : 8;
-                        const int gi = j / GS, from_lane = (lane & 28) | (gi & 3);
+                };
+                load(0, ahead[0]);
+                asm volatile("cp.async.wait_group %0;" ::"n"(STAGES - 1) : "memory");
+                __syncwarp();
+                float part[RW][NT][4];
 #pragma unroll
-                        for (int r = 0; r < RW; ++r) {
-                            const float s0 = __shfl_sync(0xffffffffu, NmType<T>::to_f(sc[r][0][gi / 4 % (8 / Q)]), from_lane);
-                            const float s1 = __shfl_sync(0xffffffffu, NmType<T>::to_f(sc[r][1][gi / 4 % (8 / Q)]), from_lane);
+                for (int j = 0; j < 8; ++j) {
+                    if (j % CJ == 0 && j + CJ < 8) load(j + CJ, ahead[(j / CJ + 1) & 1]);
+                    if (FULL || j < steps) {   // the same for the whole warp
+                        uint32_t x[NT][TERMS][4];
+                        if constexpr (STAGED) {
 #pragma unroll
                             for (int n = 0; n < NT; ++n)
 #pragma unroll
-                                for (int i = 0; i < 4; ++i) sum[r][n][i] = __fmaf_rn(i < 2 ? s0 : s1, part[r][n][i], sum[r][n][i]);
+                                for (int s = 0; s < TERMS; ++s) {
+                                    const uint4 v = reinterpret_cast<const uint4*>(frags + j * FRAG + (n * TERMS + s) * 512)[lane];
+                                    x[n][s][0] = v.x, x[n][s][1] = v.y, x[n][s][2] = v.z, x[n][s][3] = v.w;
+                                }
+                        } else {
+                            ahead[(j / CJ) & 1][j % CJ].pairs(x[0]);
+                        }
+                        if (j % GS == 0) {
+#pragma unroll
+                            for (int r = 0; r < RW; ++r)
+#pragma unroll
+                                for (int n = 0; n < NT; ++n)
+#pragma unroll
+                                    for (int i = 0; i < 4; ++i) part[r][n][i] = 0.f;
+                        }
+#pragma unroll
+                        for (int r = 0; r < RW; ++r) {
+                            const uint32_t w0 = *reinterpret_cast<const uint32_t*>(tile + (r * 16 + g) * 128 + ((j ^ g) << 4) + t * 4);
+                            const uint32_t w1 = *reinterpret_cast<const uint32_t*>(tile + (r * 16 + g + 8) * 128 + ((j ^ g) << 4) + t * 4);
+                            uint32_t lo[4], hi[4];
+                            w4_pairs(w0, lo, Mma());
+                            w4_pairs(w1, hi, Mma());
+#pragma unroll
+                            for (int p = 0; p < 4; p += 2) {
+                                const uint32_t f[4] = {lo[p], hi[p], lo[p + 1], hi[p + 1]};
+#pragma unroll
+                                for (int n = 0; n < NT; ++n)
+#pragma unroll
+                                    for (int s = 0; s < TERMS; ++s) w4_mma(part[r][n], f, x[n][s][p], x[n][s][p + 1], Mma());
+                            }
+                        }
+                        if (j % GS == GS - 1) {   // a group ends
+                            const int gi = j / GS, from_lane = (lane & 28) | (gi & 3);
+#pragma unroll
+                            for (int r = 0; r < RW; ++r) {
+                                const float s0 = __shfl_sync(0xffffffffu, NmType<T>::to_f(sc[r][0][gi >> 2]), from_lane);
+                                const float s1 = __shfl_sync(0xffffffffu, NmType<T>::to_f(sc[r][1][gi >> 2]), from_lane);
+#pragma unroll
+                                for (int n = 0; n < NT; ++n)
+#pragma unroll
+                                    for (int i = 0; i < 4; ++i) sum[r][n][i] = __fmaf_rn(i < 2 ? s0 : s1, part[r][n][i], sum[r][n][i]);
+                            }
                         }
                     }
                 }
-            }
-        };
-        if (steps == 8) block(std::true_type());
-        else block(std::false_type());
-        __syncwarp();   // the stage may be filled again
-        stage = stage == STAGES - 1 ? 0 : stage + 1;
+            };
+            if (steps == 8) block(std::true_type());
+            else block(std::false_type());
+            __syncwarp();   // the stage may be filled again
+            stage = stage == STAGES - 1 ? 0 : stage + 1;
+        }
+        if constexpr (STAGED) {
+            half ^= 1;
+            if (slice + (int)ctas < slices) lay_out(half);
+            __syncthreads();
+        }
     }
     asm volatile("cp.async.wait_group 0;" ::: "memory");
     __syncwarp();
 
     // each warp's sums to its own ring, [token][row]
-    float* mine = reinterpret_cast<float*>(ring);
+    float* own = reinterpret_cast<float*>(ring);
 #pragma unroll
     for (int r = 0; r < RW; ++r)
 #pragma unroll
         for (int n = 0; n < NT; ++n)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) mine[(n * 8 + 2 * t + (i & 1)) * PITCH + r * 16 + g + (i >> 1) * 8] = sum[r][n][i];
-    if (ctas > 1) nm_cluster_sync();
-    else __syncthreads();
-    const int rows = 16 * RW * a.row_warps;
-    for (int x = (int)rank * W4_THREADS + threadIdx.x; x < rows * NT * 8; x += (int)ctas * W4_THREADS) {
-        const int row = x % rows, m = x / rows;
-        const int64_t n = block_row + row, tok = m0 + m;
-        if (n >= d.N || tok >= d.M) continue;
-        const int at = (row / (16 * RW)) * RING + (m * PITCH + row % (16 * RW)) * 4;
-        float y = 0.f;
-        for (uint32_t c = 0; c < ctas; ++c) {
-            const uint32_t base = nm_mapa(nm_smem_u32(w4_smem + at), c);
-            for (int k = 0; k < k_warps; ++k) {
-                float v;
-                asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(base + k * a.row_warps * RING) : "memory");
-                y += v;
-            }
-        }
-        if (d.bias) y += d.bias[n];
+            for (int i = 0; i < 4; ++i) own[(n * 8 + 2 * t + (i & 1)) * PITCH + r * 16 + g + (i >> 1) * 8] = sum[r][n][i];
+    __syncthreads();
+    // The block's warps are added up first, each sum where the first of them has it, then the cluster's blocks.  A thread has one row and
+    // every so manieth token.
+    const int rows = 16 * RW * a.row_warps, row = threadIdx.x & (rows - 1), apart = W4_THREADS / rows;
+    const int tokens = d.M - m0 < NT * 8 ? (int)(d.M - m0) : NT * 8;
+    const int64_t n = block_row + row;
+    float* at = reinterpret_cast<float*>(w4_smem + (row / (16 * RW)) * RING) + row % (16 * RW);
+    const int next_warp = a.row_warps * (RING / 4);
+    const bool live = n < d.N;
+    const float bias = live && d.bias ? d.bias[n] : 0.f;
+    auto store = [&](int m, float y, float residual) {
+        if (d.bias) y += bias;
         if (a.tab) {
             const float2 kb = a.tab->kb[nm_pwl_index(y, a.tab->inv_h, a.tab->off, (float)(a.tab->n - 1))];
             y = __fmaf_rn(kb.x, y, kb.y);
         }
-        if (d.residual) y += NmType<T>::to_f(((const T*)d.residual)[tok * d.ldr + n]);
-        ((T*)d.out)[tok * d.ldo + n] = NmType<T>::from_f(y);
+        if (d.residual) y += residual;
+        ((T*)d.out)[(m0 + m) * d.ldo + n] = NmType<T>::from_f(y);
+    };
+    auto residual_of = [&](int m) { return live && d.residual && m < tokens ? NmType<T>::to_f(((const T*)d.residual)[(m0 + m) * d.ldr + n]) : 0.f; };
+#pragma unroll 4
+    for (int m = threadIdx.x / rows; m < tokens; m += apart) {
+        const float r = ctas == 1 ? residual_of(m) : 0.f;
+        float y = at[m * PITCH];
+        for (int k = 1; k < k_warps; ++k) y += at[m * PITCH + k * next_warp];
+        if (ctas > 1) at[m * PITCH] = y;
+        else if (live) store(m, y, r);
     }
-    if (ctas > 1) nm_cluster_sync();   // no CTA leaves while another reads its shared memory
+    if (ctas == 1) return;
+    nm_cluster_sync();
+    if (live) {
+        const uint32_t here = nm_smem_u32(at);
+        for (int m = (int)rank * apart + threadIdx.x / rows; m < tokens; m += (int)ctas * apart) {
+            const float r = residual_of(m);
+            float v[8], y = 0.f;
+#pragma unroll
+            for (int c = 0; c < 8; ++c)
+                if (c < (int)ctas) asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v[c]) : "r"(nm_mapa(here + m * (PITCH * 4), c)) : "memory");
+#pragma unroll
+            for (int c = 0; c < 8; ++c)
+                if (c < (int)ctas) y += v[c];
+            store(m, y, r);
+        }
+    }
+    nm_cluster_sync();   // no CTA leaves while another reads its shared memory
 }
 
 template <typename T, int NT, int RW, int GS>
 nm_status launch(nm_ctx* ctx, const nm_linear_w4_desc* d, cudaStream_t st)
 {
-    constexpr int STAGES = RW == 1 ? 4 : 3, SMEM = W4_WARPS * STAGES * RW * W4_TILE;
+    constexpr bool STAGED = NT > 1;
+    constexpr int STAGES = RW == 2 ? 3 : STAGED ? 3 : 4;
     W4Args a;
     a.d = *d;
     a.tab = d->slot == NM_SLOT_NONE ? nullptr : ctx->d_tables + d->slot;
     a.k_groups = (int)(d->K / d->group);
     a.k_blocks = (int)((d->K + W4_BLOCK_K - 1) / W4_BLOCK_K);
     const int64_t token_blocks = (d->M + NT * 8 - 1) / (NT * 8), row_tiles = (d->N + 16 * RW - 1) / (16 * RW);
-    // A block reads its tokens' activations once for all its rows: as many rows as keep those bytes below the weights' (4 M / rows).
-    // Below that, fewer row warps (and more that split k) as long as the blocks do not fill two to an SM and every warp has a block of k.
-    const int64_t tokens = d->M < NT * 8 ? d->M : NT * 8, slots = (int64_t)ctx->sm_count * 2;
+    const int64_t slots = (int64_t)ctx->sm_count * 2;
+    // As many warps along the rows as there are; fewer (and more that split k) as long as the blocks do not fill two to an SM and every
+    // warp has a block of k, and the activations' bytes that a block reads stay below the weights' (4 M / rows; STAGED: and fit).
     int rw = 8;
-    while (rw > 1 && 16 * RW * (rw / 2) >= 4 * tokens && W4_WARPS / rw < a.k_blocks && (row_tiles + rw - 1) / rw * token_blocks < slots) rw /= 2;
+    while (rw > (STAGED ? 2 * NT : 1) && 16 * RW * (rw / 2) >= 4 * d->M && W4_WARPS / rw < a.k_blocks && (row_tiles + rw - 1) / rw * token_blocks < slots) rw /= 2;
+    const int smem = W4_WARPS * STAGES * RW * W4_TILE + (STAGED ? 2 * (W4_WARPS / rw) * 8 * NT * W4Type<T>::TERMS * 512 : 0);
     a.row_warps = rw;
     a.row_blocks = (int)((row_tiles + rw - 1) / rw);
     const int64_t units = a.row_blocks * token_blocks;
@@ -353,9 +433,9 @@ nm_status launch(nm_ctx* ctx, const nm_linear_w4_desc* d, cudaStream_t st)
     while (ctas < 8 && units * ctas * 2 <= slots && a.k_blocks >= 2 * ctas * (W4_WARPS / rw)) ctas *= 2;
     if (units * ctas > INT32_MAX) return NM_ERR_SHAPE;
     auto kernel = linear_w4_kernel<T, NT, RW, STAGES, GS>;
-    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM) != cudaSuccess) return NM_ERR_CUDA;
+    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess) return NM_ERR_CUDA;
     NmLaunchScope scope(ctx, NM_KERNEL_LINEAR_W4, 0.5 * d->N * d->K, st);
-    NmLaunchConfig lc(ctx, dim3((unsigned)(units * ctas)), W4_THREADS, SMEM, st, ctas);
+    NmLaunchConfig lc(ctx, dim3((unsigned)(units * ctas)), W4_THREADS, smem, st, ctas);
     return cudaLaunchKernelEx(&lc.cfg, kernel, a) == cudaSuccess ? NM_OK : NM_ERR_CUDA;
 }
 
@@ -364,8 +444,8 @@ nm_status by_tokens(nm_ctx* ctx, const nm_linear_w4_desc* d, cudaStream_t st)
 {
     // one tile of weight rows per warp where the activations are few beside them, two otherwise (each then serves two products)
     if (d->M <= 8) return launch<T, 1, sizeof(T) == 4 ? 2 : 1, GS>(ctx, d, st);
-    if (d->M <= 16) return launch<T, 2, 2, GS>(ctx, d, st);
-    return launch<T, 4, 2, GS>(ctx, d, st);
+    if (d->M <= 16) return launch<T, 2, 1, GS>(ctx, d, st);
+    return launch<T, 4, 1, GS>(ctx, d, st);
 }
 template <typename T>
 nm_status dispatch(nm_ctx* ctx, const nm_linear_w4_desc* d, cudaStream_t st)
