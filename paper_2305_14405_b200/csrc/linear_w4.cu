@@ -78,11 +78,6 @@ template <typename T> struct W4Raw {
 #pragma unroll
         for (int i = 0; i < VECS; ++i) v[i] = __ldg(reinterpret_cast<const uint4*>(x) + i);
     }
-    __device__ __forceinline__ void zero()
-    {
-#pragma unroll
-        for (int i = 0; i < VECS; ++i) v[i] = make_uint4(0, 0, 0, 0);
-    }
     __device__ __forceinline__ void pairs(uint32_t (&p)[TERMS][4]) const
     {
         if constexpr (TERMS == 1) {
@@ -150,10 +145,10 @@ __global__ void __launch_bounds__(W4_THREADS, 2) linear_w4_kernel(const W4Args a
     // 16-byte piece c of a row lies at place c ^ (row & 7): word reads hit all banks.  Rows behind the last one are read as its copy, their
     // sums are not stored.
     const int copy_row = lane >> 3, copy_chunk = lane & 7;
-    const uint8_t* from = d.codes + (n0 + copy_row < d.N ? n0 + copy_row : d.N - 1) * d.ld_codes + copy_chunk * 16;
-    int down[RW * 4];   // rows from there to row r * 4 + copy_row
+    const uint8_t* from[RW * 4];
 #pragma unroll
-    for (int r = 0; r < RW * 4; ++r) down[r] = n0 + copy_row >= d.N ? 0 : n0 + copy_row + r * 4 < d.N ? r * 4 : (int)(d.N - 1 - n0 - copy_row);
+    for (int r = 0; r < RW * 4; ++r)
+        from[r] = d.codes + (n0 + r * 4 + copy_row < d.N ? n0 + r * 4 + copy_row : d.N - 1) * d.ld_codes + copy_chunk * 16;
     const uint32_t to[2] = {ring_at + copy_row * 128 + ((copy_chunk ^ copy_row) << 4), ring_at + (copy_row + 4) * 128 + ((copy_chunk ^ (copy_row + 4)) << 4)};
     auto fetch = [&](int b, int stage) {
         if (b < a.k_blocks) {
@@ -161,7 +156,7 @@ __global__ void __launch_bounds__(W4_THREADS, 2) linear_w4_kernel(const W4Args a
             const bool valid = b + 1 < a.k_blocks || (at + copy_chunk * 16) * 2 < d.K;   // the last block may be short
 #pragma unroll
             for (int r = 0; r < RW * 4; ++r)
-                w4_copy(to[r & 1] + (r >> 1) * 1024 + stage * (RW * W4_TILE), valid ? from + down[r] * d.ld_codes + at : d.codes, valid);
+                w4_copy(to[r & 1] + (r >> 1) * 1024 + stage * (RW * W4_TILE), valid ? from[r] + at : d.codes, valid);
         }
         asm volatile("cp.async.commit_group;" ::: "memory");
     };
@@ -204,13 +199,9 @@ __global__ void __launch_bounds__(W4_THREADS, 2) linear_w4_kernel(const W4Args a
 #pragma unroll
         for (int h = 0; h < 2; ++h) sc_next[r][h][0] = sc_next[r][h][1] = NmType<T>::from_f(0.f);
     look(first);
-    const T* acts[NT];
-    bool token[NT];
+    const T* acts[NT];   // (tokens behind the last one are read as its copy, their sums are not stored)
 #pragma unroll
-    for (int n = 0; n < NT; ++n) {
-        token[n] = m0 + n * 8 + g < d.M;
-        acts[n] = (const T*)d.A + (token[n] ? (m0 + n * 8 + g) * d.lda : 0) + t * 8;
-    }
+    for (int n = 0; n < NT; ++n) acts[n] = (const T*)d.A + (m0 + n * 8 + g < d.M ? m0 + n * 8 + g : d.M - 1) * d.lda + t * 8;
     // STAGED: warp w lays out step w of each of the slice's k_warps blocks (at most 4 / NT)
     constexpr int SLOTS = STAGED ? 4 / NT : 1;
     W4Raw<T> mine[SLOTS][NT];
@@ -220,9 +211,8 @@ __global__ void __launch_bounds__(W4_THREADS, 2) linear_w4_kernel(const W4Args a
         for (int k = 0; k < SLOTS; ++k)
 #pragma unroll
             for (int n = 0; n < NT; ++n) {
-                mine[k][n].zero();
                 const int64_t at = ((int64_t)slice * k_warps + k) * W4_BLOCK_K + warp * 32;
-                if (k < k_warps && token[n] && at < d.K) mine[k][n].load(acts[n] + at);
+                if (k < k_warps) mine[k][n].load(acts[n] + (at < d.K ? at : 0));   // (what lies behind K is not used)
             }
     };
     auto lay_out = [&](int half) {
@@ -276,8 +266,7 @@ __global__ void __launch_bounds__(W4_THREADS, 2) linear_w4_kernel(const W4Args a
                     if constexpr (!STAGED) {
 #pragma unroll
                         for (int j = 0; j < CJ; ++j) {
-                            x[j].zero();
-                            if (token[0] && (FULL || j0 + j < steps)) x[j].load(acts[0] + k0 + (j0 + j) * 32);
+                            x[j].load(acts[0] + (FULL || j0 + j < steps ? k0 + (j0 + j) * 32 : 0));
                         }
                     }
                 };
@@ -443,7 +432,7 @@ template <typename T, int GS>
 nm_status by_tokens(nm_ctx* ctx, const nm_linear_w4_desc* d, cudaStream_t st)
 {
     // one tile of weight rows per warp where the activations are few beside them, two otherwise (each then serves two products)
-    if (d->M <= 8) return launch<T, 1, sizeof(T) == 4 ? 2 : 1, GS>(ctx, d, st);
+    if (d->M <= 8) return sizeof(T) == 4 || d->N >= 32 * 2 * ctx->sm_count ? launch<T, 1, 2, GS>(ctx, d, st) : launch<T, 1, 1, GS>(ctx, d, st);
     if (d->M <= 16) return launch<T, 2, 1, GS>(ctx, d, st);
     return launch<T, 4, 1, GS>(ctx, d, st);
 }
