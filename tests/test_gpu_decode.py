@@ -411,3 +411,193 @@ def test_linear_w4_large_and_non_finite_activations(ctx, dtype):
     check(out[:2], y, dy, td)
     assert torch.isnan(out[2]).sum() >= N - 4 or torch.isnan(out[2]).all()
     assert torch.isinf(out[3]).all()
+
+
+# ---------------------------------------------------------------- rows of every kind in one call
+
+
+@pytest.mark.parametrize("dtype,hq,hk,d", [("bf16", 4, 1, 128), ("f16", 12, 1, 64), ("f32", 4, 2, 64), ("bf16", 3, 3, 40)])
+def test_attention_many_short_rows_where_long_ones_may_come(ctx, dtype, hq, hk, d):
+    """max_len says 20000, so the rows take equal shares; 300 of up to 200 tokens: several rows to a block, rows in two blocks, empty ones."""
+    td, gen = TYPES[dtype], gen_of(31)
+    lens = [int(n) for n in np.random.default_rng(5).integers(0, 201, 300)]
+    lens[0] = lens[17] = lens[18] = lens[299] = 0
+    lens[40] = 9000
+    kc, vc, tables, k, v = make_cache(gen, td, lens, 32, hk, d, "token")
+    wide = torch.full((300, 700), -5, dtype=torch.int32, device="cuda")
+    wide[:, :tables.shape[1]] = tables
+    q = randn(gen, 300, hq, d).to(td)
+    out = torch.full_like(q, 5.0)
+    desc = ctx.attn_paged_desc(q, kc, vc, wide, i32(lens), out, max_len=20000)
+    ctx.attention_pwl_paged(desc, torch.full((ctx.attention_paged_workspace_bytes(desc),), 255, dtype=torch.uint8, device="cuda"))
+    ctx.check_device_status()
+    some = [0, 1, 2, 17, 18, 39, 40, 41, 100, 255, 256, 257, 298, 299]
+    for i in some:
+        check_attention(ctx, q[i:i + 1], [k[i]], [v[i]], out[i:i + 1], [lens[i]], hq, hk, d, td)
+    # every row alone gives what it gives among the others, up to the order of its sums
+    assert torch.isfinite(out.float()).all() and not (out == 5).all(-1).any()
+
+
+@pytest.mark.parametrize("max_len", [64, 20000])
+def test_attention_of_empty_requests(ctx, max_len):
+    q = randn(gen_of(1), 3, 4, 64).bfloat16()
+    cache = torch.full((2, 16, 2, 64), float("nan"), dtype=torch.bfloat16, device="cuda")
+    out = torch.full_like(q, 5.0)
+    desc = ctx.attn_paged_desc(q, cache, cache, torch.full((3, 1250), -1, dtype=torch.int32, device="cuda"), i32([0, 0, 0]), out, max_len=max_len)
+    ctx.attention_pwl_paged(desc, torch.empty(ctx.attention_paged_workspace_bytes(desc), dtype=torch.uint8, device="cuda"))
+    ctx.check_device_status()
+    assert (out == 0).all()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_attention_score_ranges(ctx, dtype):
+    """Large scores of both signs: the maximum is the whole row's, whichever block, warp or lane has it, and values below the table's range
+    take its first line."""
+    hq, hk, d, td, n = 2, 1, 64, TYPES[dtype], 700
+    gen = gen_of(77)
+    for at in (0, 15, 16, 300, n - 1):
+        kc, vc, tables, k, v = make_cache(gen, td, [n], 16, hk, d, "token")
+        q = (4 * randn(gen, 1, hq, d)).to(td)
+        k[0] *= 0.2
+        k[0][at] = (q[0, 0] * 1.5).to(td)                      # far above all others for head 0
+        j = torch.arange(n, device="cuda")
+        row = tables[0].long()[j // 16]
+        kc[row, j % 16] = k[0]
+        out = torch.empty_like(q)
+        desc = ctx.attn_paged_desc(q, kc, vc, tables, i32([n]), out)
+        ctx.attention_pwl_paged(desc, torch.empty(ctx.attention_paged_workspace_bytes(desc), dtype=torch.uint8, device="cuda"))
+        ctx.check_device_status()
+        check_attention(ctx, q, k, v, out, [n], hq, hk, d, td)
+
+
+def test_attention_two_calls_at_once(ctx):
+    """Two streams, a workspace each, the form with equal shares: what each gives alone."""
+    hq, hk, d, td, lens = 8, 2, 128, torch.bfloat16, [15000, 3000, 1, 12000]
+    calls = []
+    for seed in (1, 2):
+        gen = gen_of(seed)
+        kc, vc, tables, k, v = make_cache(gen, td, lens, 16, hk, d, "token")
+        q = randn(gen, 4, hq, d).to(td)
+        out = torch.empty_like(q)
+        desc = ctx.attn_paged_desc(q, kc, vc, tables, i32(lens), out)
+        calls.append((desc, torch.empty(ctx.attention_paged_workspace_bytes(desc), dtype=torch.uint8, device="cuda"), out))
+    alone = []
+    for desc, ws, out in calls:
+        ctx.attention_pwl_paged(desc, ws)
+        alone.append(out.clone())
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    for _ in range(20):
+        for (desc, ws, out), s in zip(calls, streams):
+            ctx.attention_pwl_paged(desc, ws, stream=s)
+    torch.cuda.synchronize()
+    ctx.check_device_status()
+    for (_, _, out), want in zip(calls, alone):
+        assert torch.equal(out, want)
+
+
+# ---------------------------------------------------------------- a decoder's layer, step by step
+
+
+class Layer:
+    """Projection, head norms and rotation into the cache, attention, output projection of one layer with 4-bit weights, on arrays that
+    stay the same from step to step, as a captured graph wants them."""
+
+    def __init__(self, nm, ctx, seed, B, hq, hk, d, td, page=16, width=40, max_tokens=64):
+        gen = gen_of(seed)
+        H, rows = hq * d, (hq + 2 * hk) * d
+        self.nm, self.ctx, self.B, self.hq, self.hk, self.d, self.td, self.page, self.H = nm, ctx, B, hq, hk, d, td, page, H
+        pages = 3 * B + 60
+        empty = lambda *s: torch.empty(s, dtype=torch.int32, device="cuda")  # noqa: E731
+        self.lengths, self.new = torch.zeros(B, dtype=torch.int32, device="cuda"), empty(B)
+        self.tables, self.free, self.count = torch.full((B, width), -1, dtype=torch.int32, device="cuda"), torch.randperm(pages, generator=gen, device="cuda").to(torch.int32), i32([pages])
+        self.start, self.slots, self.positions = empty(B + 1), empty(max_tokens), empty(max_tokens)
+        self.kc, self.vc = (torch.full((pages, page, hk, d), float("nan"), dtype=td, device="cuda") for _ in range(2))
+        angle = torch.arange(width * page, device="cuda")[:, None] * 0.01 ** (torch.arange(d // 2, device="cuda") / (d // 2))
+        self.cos_sin = torch.cat([angle.cos(), angle.sin()], 1).float()
+        self.gq, self.gk = 1 + 0.1 * randn(gen, d), 1 + 0.1 * randn(gen, d)
+        weight = lambda n, k: (torch.randint(0, 256, (n, k // 2), generator=gen, device="cuda", dtype=torch.uint8),  # noqa: E731
+                               ((1 + 0.1 * randn(gen, n, k // 64)) * 0.2 / k ** 0.5).to(td))
+        self.wqkv, self.wo = weight(rows, H), weight(H, H)
+        self.bias = 0.1 * randn(gen, rows)
+        act = lambda n, w: torch.zeros((n, w), dtype=td, device="cuda")  # noqa: E731
+        self.x, self.qkv, self.q, self.a, self.y = act(max_tokens, H), act(max_tokens, rows), act(max_tokens, H), act(B, H), act(B, H)
+        self.plan = ctx.kv_plan_desc(self.lengths, self.new, self.tables, self.free, self.count, page, self.lengths, self.count, self.start, self.slots, self.positions)
+        self.proj = ctx.linear_w4_desc(self.x, *self.wqkv, self.qkv, bias=self.bias)
+        self.rope = ctx.qk_rope_desc(self.qkv, hq, hk, d, self.q, positions=self.positions, cos_sin=self.cos_sin, gamma_q=self.gq, gamma_k=self.gk,
+                                     k_cache=self.kc, v_cache=self.vc, slots=self.slots)
+        # (a step that adds one token to every request has them in the requests' order)
+        self.attn = ctx.attn_paged_desc(self.q[:B].view(B, hq, d), self.kc, self.vc, self.tables, self.lengths, self.a.view(B, hq, d))
+        self.ws = torch.empty(ctx.attention_paged_workspace_bytes(self.attn), dtype=torch.uint8, device="cuda")
+        self.out = ctx.linear_w4_desc(self.a, *self.wo, self.y, residual=self.x[:B])
+
+    def fill(self):
+        """Prompts: keys and values of several tokens a request."""
+        self.ctx.kv_plan(self.plan)
+        self.ctx.linear_pwl_w4(self.proj)
+        self.ctx.qk_norm_rope_pwl(self.rope)
+
+    def step(self):
+        self.fill()
+        self.ctx.attention_pwl_paged(self.attn, self.ws)
+        self.ctx.linear_pwl_w4(self.out)
+
+    def state(self):
+        return [t.clone() for t in (self.lengths, self.tables, self.free, self.count, self.start, self.slots, self.positions, self.kc.nan_to_num(7.0),
+                                    self.vc.nan_to_num(7.0), self.qkv, self.q, self.a, self.y)]
+
+
+@pytest.mark.parametrize("dtype,hq,hk,d", [("bf16", 4, 2, 64), ("f16", 8, 1, 128), ("f32", 2, 2, 64)])
+def test_decoding_steps_eager_and_captured(nm, ctx, dtype, hq, hk, d):
+    td, B = TYPES[dtype], 6
+    eager, graphed = (Layer(nm, ctx, 9, B, hq, hk, d, td) for _ in range(2))
+    prompts = [5, 16, 1, 20, 13, 9]
+    for layer in (eager, graphed):
+        layer.new.copy_(i32(prompts))
+        layer.x.copy_(randn(gen_of(50), *layer.x.shape))
+        layer.fill()
+    assert eager.lengths.tolist() == prompts
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    graphed.new.fill_(1)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):   # the calls go to the capturing stream
+        graphed.step()
+    for n in range(20):
+        new = [1] * B
+        if n == 7:
+            new[3] = -1                          # request 3 ends ...
+        if n == 8:
+            new[3] = 1                           # ... and another one takes its place
+        for layer in (eager, graphed):
+            layer.new.copy_(i32(new))
+            layer.x.copy_(randn(gen_of(100 + n), *layer.x.shape))
+        if n == 7:                               # tokens and requests are not one to one in this step: the cache alone is filled
+            eager.fill(), graphed.fill()
+        else:
+            eager.step()
+            graph.replay()
+        torch.cuda.synchronize()
+        ctx.check_device_status()
+        for s, t in zip(eager.state(), graphed.state()):
+            assert torch.equal(s, t), n
+    # the last step stage by stage, each from what the one before it has left
+    L, T = eager, B
+    y, dy = ref.linear_w4(f64(L.x), L.wqkv[0].cpu().numpy(), f64(L.wqkv[1]), f64(L.bias), None, None)
+    check(L.qkv, y, dy, td, "projection")
+    x, pos = f64(L.qkv).reshape(-1, hq + 2 * hk, d)[:T], L.positions.cpu().numpy()[:T]
+    assert pos.tolist() == [n - 1 for n in L.lengths.tolist()]
+    q, dq = ref.rope(x[:, :hq], pos, f64(L.cos_sin), f64(L.gq), 1e-6, d, False, ctx.tabs["rsqrt"])
+    check(L.q[:T], q.reshape(T, -1), dq.reshape(T, -1), td, "queries")
+    k, dk = ref.rope(x[:, hq:hq + hk], pos, f64(L.cos_sin), f64(L.gk), 1e-6, d, False, ctx.tabs["rsqrt"])
+    at = L.slots[:T].long()
+    check(L.kc[at // 16, at % 16], k, dk, td, "keys")
+    lens = L.lengths.tolist()
+    rows = [L.tables[i].long()[torch.arange(n, device="cuda") // 16] for i, n in enumerate(lens)]
+    place = [torch.arange(n, device="cuda") % 16 for n in lens]
+    check_attention(ctx, L.q[:T].view(T, hq, d), [L.kc[r, p] for r, p in zip(rows, place)], [L.vc[r, p] for r, p in zip(rows, place)], L.a.view(T, hq, d), lens, hq,
+                    hk, d, td)
+    y, dy = ref.linear_w4(f64(L.a), L.wo[0].cpu().numpy(), f64(L.wo[1]), None, f64(L.x[:B]), None)
+    check(L.y, y, dy, td, "output")
+    assert len(set(torch.cat(rows).tolist())) == sum(-(-n // 16) for n in lens)   # no page has two owners
