@@ -310,6 +310,7 @@ class Context:
         h = C.c_void_p()
         _check(self._lib.nm_ctx_create(C.byref(h), int(device)), "nm_ctx_create")
         self._h = h
+        self._raw_stream = None
         self.device = device
 
     def close(self):
@@ -324,8 +325,14 @@ class Context:
             pass
 
     def _stream(self, stream):
-        """The given stream, or the current one of the context's device."""
-        return C.c_void_p((stream if stream is not None else _torch().cuda.current_stream(self.device)).cuda_stream)
+        """The given stream, or the current one of the context's device (asked for without making a Stream object: a decoding step's calls
+        take a few microseconds each)."""
+        if stream is not None:
+            return stream.cuda_stream
+        if self._raw_stream is None:
+            torch = _torch()
+            self._raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda device: torch.cuda.current_stream(device).cuda_stream)
+        return self._raw_stream(self.device)
 
     # -- tables -------------------------------------------------------------------
     def pwl_table_load(self, slot, n, x_min, x_max, k, b):

@@ -1074,11 +1074,12 @@ PagedLayout layout_of(const nm_attn_paged_desc* d)
 }
 
 template <typename K>
-nm_status paged_launch(nm_ctx* ctx, K kernel, const PagedArgs& a, int64_t blocks, int threads, size_t smem, int ctas, double bytes, cudaStream_t st)
+nm_status paged_launch(nm_ctx* ctx, K kernel, std::atomic<uint64_t>& allowed, const PagedArgs& a, int64_t blocks, int threads, size_t smem, int ctas,
+                       double bytes, cudaStream_t st)
 {
     if (blocks > INT32_MAX) return NM_ERR_SHAPE;
     // (48 KB are there without asking, the kernels' static arrays among them)
-    if (smem > 40 * 1024 && cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess) return NM_ERR_CUDA;
+    if (smem > 40 * 1024 && !nm_allow_smem(ctx, (const void*)kernel, 220 * 1024, allowed)) return NM_ERR_CUDA;
     NmLaunchScope scope(ctx, NM_KERNEL_ATTENTION_PAGED, bytes, st);
     NmLaunchConfig lc(ctx, dim3((unsigned)blocks), threads, smem, st, ctas);
     return cudaLaunchKernelEx(&lc.cfg, kernel, a) == cudaSuccess ? NM_OK : NM_ERR_CUDA;
@@ -1089,9 +1090,10 @@ nm_status launch(nm_ctx* ctx, const PagedArgs& a, const PagedLayout& l, cudaStre
 {
     using T = typename Core::Elem;
     const double bytes = (double)a.d.B * a.d.max_len * a.d.kv_heads * a.d.d * sizeof(T);
-    if (l.fused) return paged_launch(ctx, paged_fused_kernel<Core>, a, l.blocks, PAGED_THREADS, paged_fused_bytes<Core>(l.span), l.ctas, 2 * bytes, st);
-    const nm_status s = paged_launch(ctx, paged_scores_kernel<Core>, a, l.blocks, PAGED_THREADS, paged_split_bytes<Core>(), 1, bytes, st);
-    return s != NM_OK ? s : paged_launch(ctx, paged_values_kernel<Core>, a, l.blocks, PAGED_THREADS, paged_split_bytes<Core>(), 1, bytes, st);
+    static std::atomic<uint64_t> allowed[3];
+    if (l.fused) return paged_launch(ctx, paged_fused_kernel<Core>, allowed[0], a, l.blocks, PAGED_THREADS, paged_fused_bytes<Core>(l.span), l.ctas, 2 * bytes, st);
+    const nm_status s = paged_launch(ctx, paged_scores_kernel<Core>, allowed[1], a, l.blocks, PAGED_THREADS, paged_split_bytes<Core>(), 1, bytes, st);
+    return s != NM_OK ? s : paged_launch(ctx, paged_values_kernel<Core>, allowed[2], a, l.blocks, PAGED_THREADS, paged_split_bytes<Core>(), 1, bytes, st);
 }
 
 template <typename T>

@@ -16,6 +16,7 @@
 namespace {
 
 constexpr int W4_WARPS = 8, W4_THREADS = W4_WARPS * 32, W4_BLOCK_K = 256, W4_TILE = 2048;   // a stage of 16 rows: 128 bytes each
+constexpr int W4_MAX_SMEM = 227 * 1024;
 
 struct W4Args {
     nm_linear_w4_desc d;
@@ -422,7 +423,8 @@ nm_status launch(nm_ctx* ctx, const nm_linear_w4_desc* d, cudaStream_t st)
     while (ctas < 8 && units * ctas * 2 <= slots && a.k_blocks >= 2 * ctas * (W4_WARPS / rw)) ctas *= 2;
     if (units * ctas > INT32_MAX) return NM_ERR_SHAPE;
     auto kernel = linear_w4_kernel<T, NT, RW, STAGES, GS>;
-    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess) return NM_ERR_CUDA;
+    static std::atomic<uint64_t> allowed{0};
+    if (!nm_allow_smem(ctx, (const void*)kernel, W4_MAX_SMEM, allowed)) return NM_ERR_CUDA;
     NmLaunchScope scope(ctx, NM_KERNEL_LINEAR_W4, 0.5 * d->N * d->K, st);
     NmLaunchConfig lc(ctx, dim3((unsigned)(units * ctas)), W4_THREADS, smem, st, ctas);
     return cudaLaunchKernelEx(&lc.cfg, kernel, a) == cudaSuccess ? NM_OK : NM_ERR_CUDA;

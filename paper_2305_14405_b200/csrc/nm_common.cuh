@@ -8,6 +8,8 @@
 #include <cuda_runtime.h>
 #include <stdint.h>
 
+#include <atomic>
+
 #include "../../include/nm_b200.h"
 
 // ---------------------------------------------------------------- tables ------
@@ -865,3 +867,14 @@ struct NmDivisor {
     }
     __device__ __forceinline__ int operator()(int a) const { return mul ? (int)(__umulhi((uint32_t)a, mul) >> shift) : a; }
 };
+
+// Lets a kernel have up to `bytes` of dynamic shared memory, once per device: `done` is the launch site's record of the devices (further
+// ones are asked for every time).
+static inline bool nm_allow_smem(const nm_ctx* ctx, const void* kernel, int bytes, std::atomic<uint64_t>& done)
+{
+    const uint64_t bit = ctx->device < 64 ? (uint64_t)1 << ctx->device : 0;
+    if (done.load(std::memory_order_acquire) & bit) return true;
+    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes) != cudaSuccess) return false;
+    done.fetch_or(bit, std::memory_order_release);
+    return true;
+}

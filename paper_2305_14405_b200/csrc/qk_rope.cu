@@ -2,6 +2,8 @@
 // packed projection.  Bound by its bytes (each element is read once and written once) or, for few tokens, by latency.
 // A warp goes through its units (a token, a few of its heads) with the next ones' elements on their way to a ring in shared memory; a
 // lane copies what it will read itself, so there is no barrier.
+#include <type_traits>
+
 #include "nm_common.cuh"
 
 namespace {
@@ -355,9 +357,13 @@ nm_status launch(nm_ctx* ctx, const nm_qk_rope_desc* d, cudaStream_t st)
     a.by_page = NmDivisor::of(d->k_cache ? d->page_size : 1);
     NmLaunchScope scope(ctx, NM_KERNEL_QK_ROPE, 2.0 * d->T * (d->heads + 2.0 * d->kv_heads) * d->d * sizeof(T), st);
     NmLaunchConfig lc(ctx, dim3((unsigned)blocks), ROPE_WARPS * 32, ROPE_WARPS * ROPE_RING, st);
-    auto kernel = d->pairs ? (lph == 4 ? qk_rope_kernel<T, 4, true> : lph == 8 ? qk_rope_kernel<T, 8, true> : qk_rope_kernel<T, 16, true>)
-                           : (lph == 4 ? qk_rope_kernel<T, 4, false> : lph == 8 ? qk_rope_kernel<T, 8, false> : qk_rope_kernel<T, 16, false>);
-    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, ROPE_WARPS * ROPE_RING) != cudaSuccess) return NM_ERR_CUDA;
+    auto kernels = [&](auto turn) {   // by the lanes of a head
+        constexpr bool PAIRS = decltype(turn)::value;
+        return lph == 4 ? qk_rope_kernel<T, 4, PAIRS> : lph == 8 ? qk_rope_kernel<T, 8, PAIRS> : qk_rope_kernel<T, 16, PAIRS>;
+    };
+    auto kernel = d->pairs ? kernels(std::true_type()) : kernels(std::false_type());
+    static std::atomic<uint64_t> allowed[6];
+    if (!nm_allow_smem(ctx, (const void*)kernel, ROPE_WARPS * ROPE_RING, allowed[(lph == 4 ? 0 : lph == 8 ? 1 : 2) + (d->pairs ? 3 : 0)])) return NM_ERR_CUDA;
     return cudaLaunchKernelEx(&lc.cfg, kernel, a) == cudaSuccess ? NM_OK : NM_ERR_CUDA;
 }
 
