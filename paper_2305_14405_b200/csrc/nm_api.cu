@@ -89,10 +89,13 @@ nm_status nm_ctx_create(nm_ctx** out, int device)
     if (!ctx) return NM_ERR_CUDA;
     memset(ctx, 0, sizeof(*ctx));
     ctx->device = device;
-    cudaDeviceProp prop;
-    if (cudaGetDeviceProperties(&prop, device) != cudaSuccess) { delete ctx; return NM_ERR_CUDA; }
-    ctx->sm_count = prop.multiProcessorCount;
-    if (prop.major != 10) { delete ctx; return NM_ERR_UNSUPPORTED; }  // kernels are built for sm_100a only
+    int major = 0;   // (two attributes, not cudaGetDeviceProperties: that takes milliseconds)
+    if (cudaDeviceGetAttribute(&ctx->sm_count, cudaDevAttrMultiProcessorCount, device) != cudaSuccess ||
+        cudaDeviceGetAttribute(&major, cudaDevAttrComputeCapabilityMajor, device) != cudaSuccess) {
+        delete ctx;
+        return NM_ERR_CUDA;
+    }
+    if (major != 10) { delete ctx; return NM_ERR_UNSUPPORTED; }  // kernels are built for sm_100a only
     if (cudaMalloc(&ctx->d_tables, sizeof(NmTable) * NM_NUM_SLOTS) != cudaSuccess) { delete ctx; return NM_ERR_CUDA; }
     if (cudaMalloc(&ctx->d_status, sizeof(int)) != cudaSuccess) { cudaFree(ctx->d_tables); delete ctx; return NM_ERR_CUDA; }
     if (cudaMalloc(&ctx->d_pool_w, 64 * 64 * 2) != cudaSuccess) { cudaFree(ctx->d_tables); cudaFree(ctx->d_status); delete ctx; return NM_ERR_CUDA; }
