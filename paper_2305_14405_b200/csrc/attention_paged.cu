@@ -6,7 +6,8 @@
 // A unit of work is a request, a key head and up to HEADS of its query heads.
 //   fused   one launch: a cluster of blocks per unit, scores in shared memory, maxima and sums exchanged within the cluster
 //   split   two launches, scores in the workspace: all units' tokens lie one after another and every block takes an equal share, so
-//           that requests of any lengths keep all SMs busy to the end; a unit that several blocks have is joined by the last of them
+//           that requests of any lengths keep all SMs busy to the end; a unit that several blocks have is joined by the last of them,
+//           or, if there are few units and so many blocks each, by a third launch
 // A block's tokens are split over its warps in tiles.  Two cores do a tile:
 //   PagedMma   16-bit types, d a multiple of 32: m16n8k16 products
 //   PagedFma   fp32 and other d: FMAs, a few lanes per token
@@ -16,6 +17,12 @@
 namespace {
 
 constexpr int PAGED_WARPS = 8, PAGED_THREADS = PAGED_WARPS * 32, PAGED_RING = 8192;   // bytes of a warp's ring
+
+// A unit that begins in a block and goes on (nh = 0: none): its last block, request and query heads, and whether it begins where the
+// block does (paged_place).
+struct PagedJoin {
+    int c1, b, h0, nh, first_place;
+};
 
 struct PagedArgs {
     nm_attn_paged_desc d;
@@ -29,6 +36,7 @@ struct PagedArgs {
     float *scores, *maxima;       // split: [B][heads][row]; [B][heads], of units that one block has
     float *part_max, *parts;      // split, two places per block: [HEADS]; [HEADS][d] and [HEADS], unit sums not yet joined
     int* tickets;                 // split: per block, how many blocks have finished the unit that begins in it and goes on
+    PagedJoin* joins;             // split, for a third launch (otherwise null): per block, the unit that begins in it and goes on
 };
 
 __device__ __forceinline__ float paged_table(const NmTable* t, float x)
@@ -861,7 +869,10 @@ __global__ void __launch_bounds__(PAGED_THREADS, paged_blocks(Core::RING)) paged
     int64_t* offsets = reinterpret_cast<int64_t*>(paged_smem + PAGED_WARPS * Core::RING) + warp * 64;
     nm_grid_dependency_wait();
     nm_grid_launch_dependents();   // what came before this launch is complete for the next one too
-    if (threadIdx.x == 0) a.tickets[blockIdx.x] = 0;
+    if (threadIdx.x == 0) {
+        a.tickets[blockIdx.x] = 0;
+        if (a.joins) a.joins[blockIdx.x].nh = 0;
+    }
     PagedShare share = paged_share(a, units);
     PagedSegment g;
     while (paged_next(a, share, units, &g)) {
@@ -1007,6 +1018,11 @@ __global__ void __launch_bounds__(PAGED_THREADS, paged_blocks(Core::RING)) paged
             }
         }
         if (!g.whole) {   // the unit's last block adds up what all of them left, in their order
+            if (a.joins) {
+                if (g.first == 0 && threadIdx.x == 0) a.joins[c0] = PagedJoin{(int)c1, u.b, u.h0, u.nh, g.from == c0 * share.share};
+                __syncthreads();   // the ring and the sums have been read
+                continue;
+            }
             __syncthreads();
             if (threadIdx.x == 0) {
                 __threadfence();
@@ -1021,8 +1037,75 @@ __global__ void __launch_bounds__(PAGED_THREADS, paged_blocks(Core::RING)) paged
     if (!waited) nm_grid_dependency_wait();   // a launch is not complete before the one it followed
 }
 
+// Joins the units that begin in a block and go on: a block per such unit's query head.  Groups of threads take every so manieth of the
+// unit's blocks, four channels a thread, eight loads in flight each; then the groups' sums are added.
+constexpr int JOIN_THREADS = 512;
+template <class Core>
+__global__ void __launch_bounds__(JOIN_THREADS) paged_join_kernel(const PagedArgs a)
+{
+    using T = typename Core::Elem;
+    __shared__ float4 s_out[JOIN_THREADS];
+    __shared__ float s_sum[JOIN_THREADS];
+    __shared__ float2 s_recip[NM_MAX_SEGMENTS];
+    const int tid = threadIdx.x, c0 = blockIdx.x / Core::HEADS, h = blockIdx.x % Core::HEADS;
+    const float inv_h = a.recip_tab->inv_h, off = a.recip_tab->off, nm1 = (float)(a.recip_tab->n - 1);
+    for (int i = tid; i < a.recip_tab->n; i += JOIN_THREADS) s_recip[i] = a.recip_tab->kb[i];
+    nm_grid_launch_dependents();
+    nm_grid_dependency_wait();
+    const PagedJoin j = a.joins[c0];
+    if (h >= j.nh) return;
+    const int d4 = a.d.d / 4, groups = JOIN_THREADS / d4, n = j.c1 - c0 + 1, x = tid % d4, stride = paged_part_floats(Core::HEADS, a.d.d);
+    float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+    float s = 0.f;
+    if (tid < groups * d4) {
+        for (int i0 = tid / d4; i0 < n; i0 += 8 * groups) {
+            float4 v[8];
+            float w[8];
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                const int i = min(i0 + k * groups, n - 1);
+                const float* p = a.parts + (int64_t)(2 * (c0 + i) + (i || j.first_place ? 0 : 1)) * stride;
+                v[k] = *reinterpret_cast<const float4*>(p + h * a.d.d + x * 4);
+                w[k] = p[Core::HEADS * a.d.d + h];
+            }
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                if (i0 + k * groups >= n) break;
+                o.x += v[k].x;
+                o.y += v[k].y;
+                o.z += v[k].z;
+                o.w += v[k].w;
+                s += w[k];
+            }
+        }
+        s_out[tid] = o;
+        s_sum[tid] = s;
+    }
+    __syncthreads();
+    if (tid >= d4) return;
+    for (int g = 1; g < groups; ++g) {
+        const float4 v = s_out[g * d4 + x];
+        o.x += v.x;
+        o.y += v.y;
+        o.z += v.z;
+        o.w += v.w;
+        s += s_sum[g * d4 + x];
+    }
+    const float2 kb = s_recip[nm_pwl_index(s, inv_h, off, nm1)];
+    const float r = __fmaf_rn(kb.x, s, kb.y);
+    T* result = (T*)a.d.out + (int64_t)j.b * a.d.ld_out + (int64_t)(j.h0 + h) * a.d.d + x * 4;
+    result[0] = NmType<T>::from_f(o.x * r);
+    result[1] = NmType<T>::from_f(o.y * r);
+    result[2] = NmType<T>::from_f(o.z * r);
+    result[3] = NmType<T>::from_f(o.w * r);
+}
+
 // ---------------------------------------------------------------- host
 
+// Units up to which a third launch joins them: each lies in so many blocks that one block takes long to add them up, and waits for the
+// last of them first.  bf16, 128 channels, joined in the second launch against a third: 1 unit of 122567 tokens 58 against 33 us, 2 of 50000
+// 35 / 31, 4 of 50000 39 / 38, 8 of 65536 65 / 66, 256 of 4096 104 / 112.
+constexpr int PAGED_JOIN_UNITS = 4;
 constexpr int PAGED_SMS = 148;   // the layout must not depend on the device: the workspace's size is asked for without one
 
 // Query heads of a unit: 16 where the tensor cores take them and the registers hold their sums, otherwise as few as cover the group.
@@ -1034,13 +1117,17 @@ int paged_heads(const nm_attn_paged_desc* d, bool mma)
 }
 // Tokens of a block of the fused form: scores take what rings of 64 KB leave of half an SM's shared memory.
 int paged_cap(int heads) { return (40 * 1024 - heads * 4 * 40) / (heads * 4) / 32 * 32; }
+// Bytes of K and V that a block of a cluster streams at most: a cluster has 8 blocks, so few units leave most SMs idle, while split
+// launches use all of them at some 15 us more.  128 channels, fused against split: bf16 4 key heads, 5000 / 9000 / 20000 tokens 12 / 17 / 29
+// against 19 / 20 / 29 us; fp32 5000 / 10000 / 20000 tokens 21 / 38 / 68 against 19 / 24 / 29 us.
+int64_t paged_cluster_bytes(bool mma) { return mma ? 1280 * 1024 : 640 * 1024; }
 bool paged_mma_supported(const nm_attn_paged_desc* d) { return d->dtype != NM_F32 && (d->d == 64 || d->d == 96 || d->d == 128 || d->d == 256); }
 
 struct PagedLayout {
-    bool mma, fused;
+    bool mma, fused, join_launch;
     int heads, blocks_per_head, ctas, span;
     int64_t units, row, blocks;
-    size_t scores, maxima, part_max, parts, tickets, total;
+    size_t scores, maxima, part_max, parts, tickets, joins, total;
 };
 PagedLayout layout_of(const nm_attn_paged_desc* d)
 {
@@ -1053,7 +1140,8 @@ PagedLayout layout_of(const nm_attn_paged_desc* d)
     const int cap = paged_cap(l.heads);
     int ctas = 1;
     while (ctas < 8 && ((d->max_len + ctas - 1) / ctas > cap || (l.units * ctas * 2 <= 2 * PAGED_SMS && d->max_len > ctas * 128))) ctas *= 2;
-    l.fused = d->max_len <= ctas * cap && (ctas == 1 || l.units * ctas <= 2 * PAGED_SMS);
+    const int64_t block_bytes = (int64_t)((d->max_len + ctas - 1) / ctas) * d->d * 2 * nm_dtype_size(d->dtype);
+    l.fused = d->max_len <= ctas * cap && (ctas == 1 || (l.units * ctas <= 2 * PAGED_SMS && block_bytes <= paged_cluster_bytes(l.mma)));
     if (l.fused) {
         l.ctas = ctas;
         l.span = ((d->max_len + ctas - 1) / ctas + 31) / 32 * 32;
@@ -1070,6 +1158,8 @@ PagedLayout layout_of(const nm_attn_paged_desc* d)
     l.part_max = take((size_t)l.blocks * 2 * l.heads * 4);
     l.parts = take((size_t)l.blocks * 2 * paged_part_floats(l.heads, d->d) * 4);
     l.tickets = take((size_t)l.blocks * 4);
+    l.join_launch = l.units <= PAGED_JOIN_UNITS;
+    if (l.join_launch) l.joins = take((size_t)l.blocks * sizeof(PagedJoin));
     return l;
 }
 
@@ -1092,8 +1182,10 @@ nm_status launch(nm_ctx* ctx, const PagedArgs& a, const PagedLayout& l, cudaStre
     const double bytes = (double)a.d.B * a.d.max_len * a.d.kv_heads * a.d.d * sizeof(T);
     static std::atomic<uint64_t> allowed[3];
     if (l.fused) return paged_launch(ctx, paged_fused_kernel<Core>, allowed[0], a, l.blocks, PAGED_THREADS, paged_fused_bytes<Core>(l.span), l.ctas, 2 * bytes, st);
-    const nm_status s = paged_launch(ctx, paged_scores_kernel<Core>, allowed[1], a, l.blocks, PAGED_THREADS, paged_split_bytes<Core>(), 1, bytes, st);
-    return s != NM_OK ? s : paged_launch(ctx, paged_values_kernel<Core>, allowed[2], a, l.blocks, PAGED_THREADS, paged_split_bytes<Core>(), 1, bytes, st);
+    nm_status s = paged_launch(ctx, paged_scores_kernel<Core>, allowed[1], a, l.blocks, PAGED_THREADS, paged_split_bytes<Core>(), 1, bytes, st);
+    if (s == NM_OK) s = paged_launch(ctx, paged_values_kernel<Core>, allowed[2], a, l.blocks, PAGED_THREADS, paged_split_bytes<Core>(), 1, bytes, st);
+    if (s == NM_OK && l.join_launch) s = paged_launch(ctx, paged_join_kernel<Core>, allowed[0], a, l.blocks * Core::HEADS, JOIN_THREADS, 0, 1, 0.0, st);
+    return s;
 }
 
 template <typename T>
@@ -1152,6 +1244,7 @@ nm_status nm_launch_attention_paged(nm_ctx* ctx, const nm_attn_paged_desc* d, vo
     a.part_max = (float*)(ws + l.part_max);
     a.parts = (float*)(ws + l.parts);
     a.tickets = (int*)(ws + l.tickets);
+    a.joins = l.join_launch ? (PagedJoin*)(ws + l.joins) : nullptr;
     switch (d->dtype) {
     case NM_F32: return dispatch<float>(ctx, a, l, st);
     case NM_BF16: return dispatch<__nv_bfloat16>(ctx, a, l, st);
