@@ -32,6 +32,7 @@ struct PagedArgs {
     int64_t page_bytes, token_bytes;      // distances of pages and tokens in the caches
     NmDivisor by_page;                    // by page_size
     int span;                     // fused: tokens that a block's shared memory holds; split: tokens that a block has at least
+    int lead;                     // split: positions without a token before each unit
     int64_t row;                  // split: scores of one head in the workspace
     float *scores, *maxima;       // split: [B][heads][row]; [B][heads], of units that one block has
     float *part_max, *parts;      // split, two places per block: [HEADS]; [HEADS][d] and [HEADS], unit sums not yet joined
@@ -757,7 +758,7 @@ __global__ void __launch_bounds__(PAGED_THREADS, paged_blocks(Core::RING)) paged
     if (ctas > 1) nm_cluster_sync();   // no block leaves while another reads its shared memory
 }
 
-// Split form.  All requests' units lie one after another, every unit's tokens as whole 32s; block i has positions [i * share, (i + 1) * share).
+// Split form.  All requests' units lie one after another (paged_width); block i has positions [i * share, (i + 1) * share).
 // Its part of one unit is a segment.  A unit that lies in several blocks has one segment in each: the block's head segment where the
 // unit covers the block's first position, its tail segment otherwise, so a block has room for the sums of two.
 struct PagedShare {
@@ -765,6 +766,9 @@ struct PagedShare {
     int b, len;                      // the current request
 };
 __device__ __forceinline__ int paged_len32(int len) { return (len + 31) & ~31; }
+
+// Positions of a unit: some without a token, for what a segment costs next to its tokens, then its tokens as whole 32s.
+__device__ __forceinline__ int64_t paged_width(const PagedArgs& a, int len) { return len ? (int64_t)a.lead + paged_len32(len) : 0; }
 
 // Length of request b for the shares: 0 where it is outside what the call was made for.
 __device__ __forceinline__ int paged_length_or_0(const PagedArgs& a, int b)
@@ -780,7 +784,7 @@ __device__ __forceinline__ PagedShare paged_share(const PagedArgs& a, int units)
     __shared__ int s_b;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     int64_t mine = 0;
-    for (int b = tid; b < a.d.B; b += PAGED_THREADS) mine += paged_len32(paged_length_or_0(a, b));
+    for (int b = tid; b < a.d.B; b += PAGED_THREADS) mine += paged_width(a, paged_length_or_0(a, b));
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) mine += __shfl_xor_sync(0xffffffffu, mine, o);
     if (lane == 0) s_warp[warp] = mine;
@@ -801,7 +805,7 @@ __device__ __forceinline__ PagedShare paged_share(const PagedArgs& a, int units)
     int64_t before = 0;   // of the requests of earlier turns
     for (int b0 = 0; b0 < a.d.B; b0 += PAGED_THREADS) {
         const int b = b0 + tid;
-        const int64_t own = b < a.d.B ? (int64_t)paged_len32(paged_length_or_0(a, b)) * units : 0;
+        const int64_t own = b < a.d.B ? paged_width(a, paged_length_or_0(a, b)) * units : 0;
         int64_t x = own;
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) {
@@ -838,16 +842,18 @@ struct PagedSegment {
 __device__ __forceinline__ bool paged_next(const PagedArgs& a, PagedShare& s, int units, PagedSegment* g)
 {
     if (s.pos >= s.end) return false;
-    int len32 = paged_len32(s.len);
-    while (s.pos >= s.row0 + (int64_t)len32 * units) {   // the next request that has tokens
-        s.row0 += (int64_t)len32 * units;
+    int64_t width = paged_width(a, s.len);
+    while (s.pos >= s.row0 + width * units) {   // the next request that has tokens
+        s.row0 += width * units;
         s.len = paged_length_or_0(a, ++s.b);
-        len32 = paged_len32(s.len);
+        width = paged_width(a, s.len);
     }
-    const int64_t local = s.pos - s.row0;
+    const int len32 = paged_len32(s.len);
     g->b = s.b;
-    g->unit = (int)(local / len32);
-    g->from = s.row0 + (int64_t)g->unit * len32;
+    g->unit = (int)((s.pos - s.row0) / width);
+    g->from = s.row0 + g->unit * width + a.lead;
+    if (s.pos < g->from) s.pos = g->from;
+    if (s.pos >= s.end) return false;   // only positions without a token were left
     g->first = (int)(s.pos - g->from);
     const int64_t stop = g->from + len32 < s.end ? g->from + len32 : s.end;
     g->count = min(s.len, (int)(stop - g->from)) - g->first;
@@ -1102,6 +1108,11 @@ __global__ void __launch_bounds__(JOIN_THREADS) paged_join_kernel(const PagedArg
 
 // ---------------------------------------------------------------- host
 
+// A segment costs a block some 4 us next to its bytes: the first pages and tokens to arrive, the warps' sums, the join.  So that blocks with
+// many short segments do not end last, each unit counts for as many bytes of K more as a block moves meanwhile.  bf16, 8 key heads of 128
+// channels, 64 requests of 1 to 4096 tokens: 0 / 32 / 64 / 96 / 128 / 256 KB 169 / 124 / 102 / 99 / 99 / 104 us; 15 requests of 0 to 2898
+// tokens 73 / 35 / 34 / 33 / 33 / 35 us; requests of 4096 tokens alike gain nothing.
+constexpr int PAGED_LEAD_BYTES = 96 * 1024;
 // Units up to which a third launch joins them: each lies in so many blocks that one block takes long to add them up, and waits for the
 // last of them first.  bf16, 128 channels, joined in the second launch against a third: 1 unit of 122567 tokens 58 against 33 us, 2 of 50000
 // 35 / 31, 4 of 50000 39 / 38, 8 of 65536 65 / 66, 256 of 4096 104 / 112.
@@ -1237,6 +1248,7 @@ nm_status nm_launch_attention_paged(nm_ctx* ctx, const nm_attn_paged_desc* d, vo
     a.page_bytes = d->stride_page * es;
     a.token_bytes = d->stride_token * es;
     a.by_page = NmDivisor::of(d->page_size);
+    a.lead = PAGED_LEAD_BYTES / (d->d * es) / 32 * 32;
     a.row = l.row;
     uint8_t* ws = (uint8_t*)workspace;
     a.scores = (float*)(ws + l.scores);
