@@ -1128,9 +1128,9 @@ int paged_heads(const nm_attn_paged_desc* d, bool mma)
 }
 // Tokens of a block of the fused form: scores take what rings of 64 KB leave of half an SM's shared memory.
 int paged_cap(int heads) { return (40 * 1024 - heads * 4 * 40) / (heads * 4) / 32 * 32; }
-// Bytes of K and V that a block of a cluster streams at most: a cluster has 8 blocks, so few units leave most SMs idle, while split
-// launches use all of them at some 15 us more.  128 channels, fused against split: bf16 4 key heads, 5000 / 9000 / 20000 tokens 12 / 17 / 29
-// against 19 / 20 / 29 us; fp32 5000 / 10000 / 20000 tokens 21 / 38 / 68 against 19 / 24 / 29 us.
+// Bytes of K and V that a block of a cluster streams at most where the clusters leave SMs idle: split launches use all SMs at some 15 us more.
+// 128 channels, fused against split: bf16 4 key heads, 5000 / 9000 / 20000 tokens 12 / 17 / 29 against 19 / 20 / 29 us; fp32 5000 / 10000 /
+// 20000 tokens 21 / 38 / 68 against 19 / 24 / 29 us.  (Where none is idle: fp32, 16 requests of 4096 tokens, 8 key heads 88 against 102 us.)
 int64_t paged_cluster_bytes(bool mma) { return mma ? 1280 * 1024 : 640 * 1024; }
 bool paged_mma_supported(const nm_attn_paged_desc* d) { return d->dtype != NM_F32 && (d->d == 64 || d->d == 96 || d->d == 128 || d->d == 256); }
 
@@ -1152,7 +1152,7 @@ PagedLayout layout_of(const nm_attn_paged_desc* d)
     int ctas = 1;
     while (ctas < 8 && ((d->max_len + ctas - 1) / ctas > cap || (l.units * ctas * 2 <= 2 * PAGED_SMS && d->max_len > ctas * 128))) ctas *= 2;
     const int64_t block_bytes = (int64_t)((d->max_len + ctas - 1) / ctas) * d->d * 2 * nm_dtype_size(d->dtype);
-    l.fused = d->max_len <= ctas * cap && (ctas == 1 || (l.units * ctas <= 2 * PAGED_SMS && block_bytes <= paged_cluster_bytes(l.mma)));
+    l.fused = d->max_len <= ctas * cap && (ctas == 1 || (l.units * ctas <= 2 * PAGED_SMS && (l.units * ctas > PAGED_SMS || block_bytes <= paged_cluster_bytes(l.mma))));
     if (l.fused) {
         l.ctas = ctas;
         l.span = ((d->max_len + ctas - 1) / ctas + 31) / 32 * 32;
