@@ -1,5 +1,8 @@
 // Norm of the heads of queries and keys (PWL rsqrt), rotation by position and write to the paged cache: one pass over the
-// packed projection.  Bound by its bytes (each element is read once and written once) or, for few tokens, by latency.
+// packed projection.  Each element is read once and written once, rounded once at the end; sums and rotation are fp32.
+// Measured: 16383 tokens of 48 heads of 128 in bf16 (407 MB) 87 us, 4.7 TB/s; 192 tokens 4.2 us; one token 3.3 us, all of it latency.
+// The large case is bound by issue: about 0.57 instructions per cycle and scheduler with half of the DRAM rate taken; without norm and
+// rotation the same moves take 70 to 75 us.
 // A warp goes through its units (a token, a few of its heads) with the next ones' elements on their way to a ring in shared memory; a
 // lane copies what it will read itself, so there is no barrier.
 #include <type_traits>
