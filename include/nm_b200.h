@@ -473,7 +473,8 @@ nm_status nm_encoder_layer_static(nm_ctx* ctx, const nm_encoder_weights* w, cons
  * and free_pages stay, all of token_start and positions is 0, all slots are -1, and the status word gets NM_ERR_WORKSPACE (too
  * few free pages), NM_ERR_SHAPE (a request longer than max_pages pages, more than max_tokens new tokens) or
  * NM_ERR_INVALID_ARG (a negative length, one of more than max_pages pages, a free_count or a released stack outside
- * [0, free_capacity]), the last named first where several hold. */
+ * [0, free_capacity]), the last named first where several hold.  A new token on a page whose slots do not fit 31 bits, or on
+ * one of a negative number, gets slot -1, and the status word NM_ERR_INVALID_ARG. */
 typedef struct {
     int32_t B, page_size, max_pages, max_tokens, free_capacity;
     const int32_t* lengths;

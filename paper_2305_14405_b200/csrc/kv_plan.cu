@@ -3,7 +3,7 @@
 // Pages and slots of a request follow from exclusive prefix sums over the requests before it: pages given back, pages wanted, tokens added.
 // One cluster does the scan (its blocks exchange totals through shared memory) and then writes the maps, so no second launch and no
 // flag in memory is needed.  A few bytes per request and 8 per new token: bound by latency (loads, scan, cluster barriers, stores).
-// Measured: 256 requests with a token each 7.2 us, 1024 requests of up to 512 new tokens 22 us, most of it the maps' 2 MB
+// Measured: 256 requests with a token each 8.0 us, 1024 requests of up to 512 new tokens 22 us, most of it the maps' 2 MB
 // through 8 SMs; a grid over all SMs would write them in 1 us but need a second launch (2 to 3 us) and steps of that size are rare.
 #include "nm_common.cuh"
 
@@ -18,6 +18,7 @@ struct PlanStep {
 struct PlanArgs {
     nm_kv_plan_desc d;
     NmDivisor by_page;
+    uint32_t pages;   // page numbers below this one have slots of 31 bits
     int* status;
     int ctas, wide;   // wide: slots and positions are 16-byte aligned
 };
@@ -212,7 +213,8 @@ __global__ void __launch_bounds__(THREADS) kv_plan_kernel(const PlanArgs p)
                                              : a.free_pages[top - page0 - (s_page[r] + entry - s_held[r])];
                     entry_of = entry;
                 }
-                slot[k] = page * a.page_size + pos - entry * a.page_size;
+                if ((uint32_t)page < p.pages) slot[k] = page * a.page_size + (pos - entry * a.page_size);
+                else atomicExch(p.status, (int)NM_ERR_INVALID_ARG);
                 position[k] = pos;
             }
             const int at = token0 + x0;
@@ -257,6 +259,7 @@ nm_status nm_launch_kv_plan(nm_ctx* ctx, const nm_kv_plan_desc* d, cudaStream_t 
     PlanArgs p;
     p.d = *d;
     p.by_page = NmDivisor::of(d->page_size);
+    p.pages = (uint32_t)((1ll << 31) / d->page_size);
     p.status = ctx->d_status;
     p.wide = nm_aligned16(d->slots) && nm_aligned16(d->positions);
     // A step of few requests and tokens is a chain of latencies: one small block (B 256: 10.8 us with 1024 threads and three scans).

@@ -117,6 +117,20 @@ def test_plan_that_cannot_be_made_changes_nothing(ctx, lengths, new, count, max_
     assert p.run_and_check() == status
 
 
+def test_plan_gives_no_slot_on_pages_that_have_none(ctx):
+    """A negative page, and one whose slots pass 31 bits (2^28 + 3 pages of 16: as 32 bits they would be page 3's)."""
+    for bad in (-1, -2 ** 31, 2 ** 27, 2 ** 28 + 3, 2 ** 31 - 1):
+        p = Plan(ctx, [0, 16, 30], [2, 3, 4], 16, 4, [7, 8, bad], 3, 12)
+        p.tables[2, 1] = bad                      # held: the first two tokens of the third request go there
+        ctx.kv_plan(p.desc)
+        assert ctx.poll_status() == 1
+        assert p.out["slots"].tolist() == [-1, -1, 128, 129, 130, -1, -1, 112, 113, -1, -1, -1]
+        assert p.out["positions"].tolist() == [0, 1, 16, 17, 18, 30, 31, 32, 33, 0, 0, 0]
+    p = Plan(ctx, [0], [2], 16, 4, [2 ** 27 - 1], 1, 2)
+    assert p.run_and_check() == 0
+    assert p.out["slots"].tolist() == [2 ** 31 - 16, 2 ** 31 - 15]
+
+
 def test_plan_of_nothing(ctx):
     p = Plan(ctx, [], [], 16, 4, range(8), 5, 6)
     assert p.run_and_check() == 0
