@@ -17,6 +17,9 @@ bool aligned4(const void* p) { return ((uintptr_t)p & 3u) == 0; }
 bool rows16(int64_t stride, size_t es) { return (stride * (int64_t)es) % 16 == 0; }
 
 // The distances of a cache's pages, tokens and heads: none negative, 16-byte rows (or a distance that is never used).
+// Counts of requests, tokens, pages and channels: the kernels step through them in 32 bits, some thousands at a time.
+constexpr int64_t DECODE_MAX = 1 << 30;
+
 nm_status check_cache(int32_t num_pages, int32_t page_size, int64_t sp, int64_t st, int64_t sh, size_t es)
 {
     if (num_pages < 1 || page_size < 1 || (int64_t)num_pages * page_size > INT32_MAX) return NM_ERR_SHAPE;
@@ -27,6 +30,8 @@ nm_status check_cache(int32_t num_pages, int32_t page_size, int64_t sp, int64_t 
 nm_status check_attn_paged(const nm_attn_paged_desc* d)
 {
     if (d->B < 0 || d->heads < 1 || d->kv_heads < 1 || d->heads % d->kv_heads || d->max_len < 0) return NM_ERR_SHAPE;
+    if (d->B > DECODE_MAX || d->max_len > DECODE_MAX || (int64_t)d->heads * d->d > INT32_MAX) return NM_ERR_SHAPE;
+    if ((double)d->B * d->heads * d->max_len > 1e15) return NM_ERR_SHAPE;   // the workspace's size fits 64 bits
     if (!float_type(d->dtype)) return NM_ERR_UNSUPPORTED;
     if (d->d < 8 || d->d > 256 || d->d % 8) return NM_ERR_SHAPE;
     if (d->max_pages < 0 || d->page_size < 1 || d->max_len > (int64_t)d->max_pages * d->page_size) return NM_ERR_SHAPE;
@@ -41,6 +46,7 @@ nm_status nm_kv_plan(nm_ctx* ctx, const nm_kv_plan_desc* d, void* stream)
 {
     if (!ctx || !d) return NM_ERR_INVALID_ARG;
     if (d->B < 0 || d->page_size < 1 || d->max_pages < 0 || d->max_tokens < 0 || d->free_capacity < 0) return NM_ERR_SHAPE;
+    if (d->B > DECODE_MAX || d->max_tokens > DECODE_MAX || d->free_capacity > DECODE_MAX) return NM_ERR_SHAPE;
     if ((int64_t)d->max_pages * d->page_size > INT32_MAX || d->ld_tables < d->max_pages) return NM_ERR_SHAPE;
     if (!d->free_count || !d->free_count_out || !d->token_start) return NM_ERR_INVALID_ARG;
     if (d->B > 0 && (!d->lengths || !d->new_tokens || !d->lengths_out)) return NM_ERR_INVALID_ARG;
@@ -58,7 +64,7 @@ nm_status nm_kv_plan(nm_ctx* ctx, const nm_kv_plan_desc* d, void* stream)
 nm_status nm_qk_norm_rope_pwl(nm_ctx* ctx, const nm_qk_rope_desc* d, void* stream)
 {
     if (!ctx || !d) return NM_ERR_INVALID_ARG;
-    if (d->T < 0 || d->heads < 0 || d->kv_heads < 0 || (int64_t)d->heads + 2 * (int64_t)d->kv_heads > INT32_MAX) return NM_ERR_SHAPE;
+    if (d->T < 0 || d->T > DECODE_MAX || d->heads < 0 || d->kv_heads < 0 || (int64_t)d->heads + 2 * (int64_t)d->kv_heads > INT32_MAX) return NM_ERR_SHAPE;
     if (!float_type(d->dtype)) return NM_ERR_UNSUPPORTED;
     if (d->d < 8 || d->d > 256 || d->d % 8) return NM_ERR_SHAPE;
     if (d->rot < 0 || d->rot > d->d || d->rot % (d->pairs ? 8 : 16)) return NM_ERR_SHAPE;
@@ -123,7 +129,7 @@ nm_status nm_attention_pwl_paged(nm_ctx* ctx, const nm_attn_paged_desc* d, void*
 nm_status nm_linear_pwl_w4(nm_ctx* ctx, const nm_linear_w4_desc* d, void* stream)
 {
     if (!ctx || !d) return NM_ERR_INVALID_ARG;
-    if (d->M < 0 || d->N < 0 || d->K < 0 || d->M > INT32_MAX || d->N > INT32_MAX || d->K > INT32_MAX) return NM_ERR_SHAPE;
+    if (d->M < 0 || d->N < 0 || d->K < 0 || d->M > DECODE_MAX || d->N > DECODE_MAX || d->K > DECODE_MAX) return NM_ERR_SHAPE;
     if (!float_type(d->dtype)) return NM_ERR_UNSUPPORTED;
     if (d->group != 32 && d->group != 64 && d->group != 128) return NM_ERR_UNSUPPORTED;
     if (d->slot != NM_SLOT_NONE) {

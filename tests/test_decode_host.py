@@ -147,6 +147,23 @@ def test_w4_of_nothing(lib, ctx):
     assert lib.nm_linear_pwl_w4(ctx, C.byref(w4_desc(N=0, codes=None)), None) == 0
 
 
+def test_counts_that_32_bit_steps_would_pass(lib, ctx):
+    big = (1 << 30) + 1
+    for name in ("B", "max_tokens", "free_capacity"):
+        assert lib.nm_kv_plan(ctx, C.byref(plan_desc(**{name: big})), None) == SHAPE
+    assert lib.nm_qk_norm_rope_pwl(ctx, C.byref(rope_desc(T=big)), None) == SHAPE
+    long = {"max_pages": 1 << 17, "page_size": 1 << 13, "ld_tables": 1 << 17}
+    for change in ({"B": big}, dict(long, max_pages=(1 << 17) + 1, ld_tables=(1 << 17) + 1, max_len=big),
+                   dict(long, max_len=1 << 30, B=1 << 18), {"heads": 1 << 25, "ld_q": 1 << 31, "ld_out": 1 << 31}):
+        d = attn_desc(**change)
+        assert lib.nm_attention_pwl_paged(ctx, C.byref(d), A, 1 << 62, None) == SHAPE
+        assert lib.nm_attention_paged_workspace_bytes(C.byref(d)) == 0
+    d = attn_desc(**dict(long, max_len=1 << 30, num_pages=1))            # the longest: scores of 2 x 8 rows and some more
+    assert 64 << 30 < lib.nm_attention_paged_workspace_bytes(C.byref(d)) < 65 << 30
+    for name in ("M", "N", "K"):
+        assert lib.nm_linear_pwl_w4(ctx, C.byref(w4_desc(**{name: 1 << 30 | 128})), None) == SHAPE
+
+
 def test_null_contexts_and_descriptors(lib, ctx):
     assert lib.nm_kv_plan(None, C.byref(plan_desc()), None) == INVALID and lib.nm_kv_plan(ctx, None, None) == INVALID
     assert lib.nm_qk_norm_rope_pwl(None, C.byref(rope_desc()), None) == INVALID and lib.nm_qk_norm_rope_pwl(ctx, None, None) == INVALID
