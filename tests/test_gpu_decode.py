@@ -452,7 +452,42 @@ def test_attention_many_short_rows_where_long_ones_may_come(ctx, dtype, hq, hk, 
     assert torch.isfinite(out.float()).all() and not (out == 5).all(-1).any()
 
 
-@pytest.mark.parametrize("max_len", [64, 20000])
+@pytest.mark.parametrize("dtype,hq,d", [("bf16", 4, 128), ("f16", 10, 64), ("f32", 3, 64), ("bf16", 2, 40)])
+@pytest.mark.parametrize("requests", [1, 4, 5])
+def test_attention_replayed_over_other_lengths(ctx, dtype, hq, d, requests):
+    """A captured call over few long rows replayed as the lengths change: sums that an earlier replay left in the
+    workspace are nobody's, a row that lay in many blocks may lie in one or have no token, a refused length leaves its output."""
+    td, gen = TYPES[dtype], gen_of(requests)
+    longest = [9001, 300, 4097, 64, 2500][:requests]
+    kc, vc, tables, k, v = make_cache(gen, td, longest, 64, 1, d, "token")
+    wide = torch.full((requests, 400), -5, dtype=torch.int32, device="cuda")
+    wide[:, :tables.shape[1]] = tables
+    q = randn(gen, requests, hq, d).to(td)
+    out, lens = torch.full_like(q, 5.0), i32(longest)
+    desc = ctx.attn_paged_desc(q, kc, vc, wide, lens, out, max_len=25000)
+    ws = torch.full((ctx.attention_paged_workspace_bytes(desc),), 255, dtype=torch.uint8, device="cuda")   # (with 40 channels none: one cluster)
+    ctx.attention_pwl_paged(desc, ws)
+    ctx.check_device_status()
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=s):
+        ctx.attention_pwl_paged(desc, ws)
+    for change in (longest, [1] * requests, [0] * requests, [(n * 7) // 9 for n in longest], [25001] + longest[1:], longest):
+        lens.copy_(i32(change))
+        out.fill_(5.0)
+        graph.replay()
+        torch.cuda.synchronize()
+        refused = change[0] > 25000
+        assert ctx.poll_status() == (2 if refused else 0)
+        if refused:
+            assert (out[0] == 5).all()
+        for i in range(1 if refused else 0, requests):
+            n = change[i]
+            check_attention(ctx, q[i:i + 1], [k[i][:n]], [v[i][:n]], out[i:i + 1], [n], hq, 1, d, td)
+
+
+@pytest.mark.parametrize("max_len", [0, 64, 20000])
 def test_attention_of_empty_requests(ctx, max_len):
     q = randn(gen_of(1), 3, 4, 64).bfloat16()
     cache = torch.full((2, 16, 2, 64), float("nan"), dtype=torch.bfloat16, device="cuda")
