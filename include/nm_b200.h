@@ -540,8 +540,8 @@ nm_status nm_qk_norm_rope_pwl(nm_ctx* ctx, const nm_qk_rope_desc* desc, void* st
  * length are not read.  A length outside [0, max_len] is recorded as NM_ERR_SHAPE in the status word and the request's
  * output left as it was.  max_len (at most max_pages*page_size) is what the launch and the workspace are sized for.
  * Q [B, heads*d], pitch ld_q; out likewise, ld_out.  dtype F32, BF16 or F16 for Q, the caches and out; fp32 scores, sums and
- * probabilities (the 16-bit types multiply probabilities into V as two terms, 16 bits of them for BF16, 22 for F16, there to
- * 2^-25 at best and up to 65504; an infinite V gives NaN then, an infinity times a second term of 0).
+ * probabilities (the 16-bit types multiply probabilities into V as three 16-bit terms that add up to the fp32 number; for F16 to 2^-45 at
+ * best and up to 65504, and there an |e| below 2^-24 gives NaN with an infinite V).
  * heads a multiple of kv_heads; d a multiple of 8, at most 256.  Pointers 16-byte aligned, strides multiples of 16 bytes.
  * workspace: device, 256-byte aligned, nm_attention_paged_workspace_bytes of it (0 on a bad descriptor); calls that may be in
  * flight together, replays of captured graphs among them, need one each. */

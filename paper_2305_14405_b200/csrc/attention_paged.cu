@@ -174,21 +174,42 @@ __device__ __forceinline__ void paged_mma(float* c, uint32_t a0, uint32_t a1, ui
         : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
         : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
-// (a, b) as a pair of 16-bit numbers and what they leave of a and b
-__device__ __forceinline__ uint32_t paged_term(float& a, float& b, __nv_bfloat16)
-{
-    const __nv_bfloat162 h = __floats2bfloat162_rn(a, b);
-    a -= __low2float(h);
-    b -= __high2float(h);
-    return *reinterpret_cast<const uint32_t*>(&h);
-}
-__device__ __forceinline__ uint32_t paged_term(float& a, float& b, __half)
-{
-    const __half2 h = __floats2half2_rn(a, b);
-    a -= __low2float(h);
-    b -= __high2float(h);
-    return *reinterpret_cast<const uint32_t*>(&h);
-}
+// Two probabilities as three packed 16-bit terms each, w[2] the largest; term number t counts LIFT^(t - 2)-fold.  Each term but the last is
+// the remainder so far rounded towards zero and, being cut from a value one unit lower, always smaller than the remainder: the next
+// one is never zero and has the same sign, so an infinite V gives an infinity and not 0 * inf.
+//   bf16   8 bits a term: the three add up to e exactly
+//   fp16   11 bits a term, but fp16 ends at 2^-24, where a row of many small probabilities has much of its sum.  So what a term leaves,
+//          at most 2^-10 of the power of two below it, is multiplied by 2^10: nothing overflows that did not before, and e is
+//          exact from 2^-21 on and to 2^-45 below (an |e| below 2^-24 has no first term: it gives NaN with an infinite V)
+template <typename T> struct PagedTerms;
+template <> struct PagedTerms<__nv_bfloat16> {
+    static constexpr float LIFT = 1.f;
+    static __device__ __forceinline__ uint32_t cut(float& a, float& b)
+    {
+        const uint32_t x = __float_as_uint(__fmul_rz(a, 0x1.fffffep-1f)), y = __float_as_uint(__fmul_rz(b, 0x1.fffffep-1f));
+        a -= __uint_as_float(x & 0xffff0000u);
+        b -= __uint_as_float(y & 0xffff0000u);
+        return __byte_perm(x, y, 0x7632);
+    }
+    static __device__ __forceinline__ uint32_t last(float a, float b) { return __byte_perm(__float_as_uint(a), __float_as_uint(b), 0x7632); }
+};
+template <> struct PagedTerms<__half> {
+    static constexpr float LIFT = 1024.f;
+    static __device__ __forceinline__ uint32_t cut(float& a, float& b)
+    {
+        uint32_t w;
+        asm("cvt.rz.f16x2.f32 %0, %1, %2;" : "=r"(w) : "f"(__fmul_rz(b, 0x1.fffffep-1f)), "f"(__fmul_rz(a, 0x1.fffffep-1f)));
+        const float2 h = __half22float2(*reinterpret_cast<const __half2*>(&w));
+        a = (a - h.x) * LIFT;
+        b = (b - h.y) * LIFT;
+        return w;
+    }
+    static __device__ __forceinline__ uint32_t last(float a, float b)
+    {
+        const __half2 h = __floats2half2_rn(a, b);
+        return *reinterpret_cast<const uint32_t*>(&h);
+    }
+};
 
 // Four 8 x 8 matrices of 16-bit numbers, lane l giving the address of row l % 8 of matrix l / 8; transposed on request.
 __device__ __forceinline__ void paged_ldmatrix(uint32_t* r, uint32_t at)
@@ -205,7 +226,7 @@ __device__ __forceinline__ void paged_ldmatrix_trans(uint32_t* r, uint32_t at)
 
 // Tiles of MT * 16 tokens, NT tiles of 8 query heads: S^T = K Q^T and O^T = V^T P^T, tokens or channels as rows, so that eight heads fill
 // a product.  Rows are copied whole and lie in the ring with their 16-byte pieces permuted, piece c of row r at c ^ (r & 7) (rows of
-// 96 channels one piece apart instead): neither the copies nor the matrix reads collide.  Probabilities are two 16-bit terms.
+// 96 channels one piece apart instead): neither the copies nor the matrix reads collide.  Probabilities are three 16-bit terms (PagedTerms).
 template <typename T, int D_, int NT> struct PagedMma {
     using Elem = T;
     static constexpr int D = D_, HEADS = NT * 8, MT = D <= 64 ? 2 : 1, TILE = 16 * MT, LANES = D / 8;   // lanes of a row
@@ -324,16 +345,14 @@ template <typename T, int D_, int NT> struct PagedMma {
         float acc[NT][D / 16][4], sum[NT], m[NT];
         float2 next[MT][NT][2];   // scores of the next tile
         // (heads behind the last one read its scores: their sums are dropped)
-        auto look = [&](int i0) {
+        auto look = [&](int n, int i0) {
 #pragma unroll
             for (int x = 0; x < MT; ++x)
 #pragma unroll
-                for (int n = 0; n < NT; ++n)
-#pragma unroll
-                    for (int r = 0; r < 2; ++r) {
-                        const int i = i0 + x * 16 + 2 * t + r * 8;   // a row's storage has whole 32s
-                        if (i < count) next[x][n][r] = get(min(n * 8 + g, nh - 1), i);
-                    }
+                for (int r = 0; r < 2; ++r) {
+                    const int i = i0 + x * 16 + 2 * t + r * 8;   // a row's storage has whole 32s
+                    if (i < count) next[x][n][r] = get(min(n * 8 + g, nh - 1), i);
+                }
         };
         paged_pipeline<STAGES, TILE>(
             count, [&](int n, int stage) { fetch(V, cursor, ring_at, n, stage); },
@@ -348,7 +367,8 @@ template <typename T, int D_, int NT> struct PagedMma {
                 }
 #pragma unroll
                 for (int y = 0; y < MT * NT * 2; ++y) next[y / (NT * 2)][y / 2 % NT][y & 1] = make_float2(0.f, 0.f);
-                look((threadIdx.x >> 5) * TILE);
+#pragma unroll
+                for (int n = 0; n < NT; ++n) look(n, (threadIdx.x >> 5) * TILE);
             },
             [&](int stage) {
 #pragma unroll
@@ -359,11 +379,12 @@ template <typename T, int D_, int NT> struct PagedMma {
             },
             [&](int i0) {
                 const bool whole = i0 + TILE <= count;
-                uint32_t hi[MT][NT][2], lo[MT][NT][2];
+                using Terms = PagedTerms<T>;
 #pragma unroll
-                for (int x = 0; x < MT; ++x)
+                for (int n = 0; n < NT; ++n) {
+                    uint32_t w[3][MT][2];
 #pragma unroll
-                    for (int n = 0; n < NT; ++n)
+                    for (int x = 0; x < MT; ++x)
 #pragma unroll
                         for (int r = 0; r < 2; ++r) {
                             float p0 = exp(next[x][n][r].x - m[n]), p1 = exp(next[x][n][r].y - m[n]);
@@ -373,21 +394,39 @@ template <typename T, int D_, int NT> struct PagedMma {
                                 p1 = i + 1 < count ? p1 : 0.f;
                             }
                             sum[n] += p0 + p1;
-                            hi[x][n][r] = paged_term(p0, p1, T());
-                            lo[x][n][r] = paged_term(p0, p1, T());
+                            w[2][x][r] = Terms::cut(p0, p1);
+                            w[1][x][r] = Terms::cut(p0, p1);
+                            w[0][x][r] = Terms::last(p0, p1);
                         }
-                look(i0 + PAGED_WARPS * TILE);
+                    look(n, i0 + PAGED_WARPS * TILE);
+                    // The tensor core truncates its sums: a tile's products have a sum of their own, smallest terms first, and are added
+                    // to those of the tiles before in fp32, rounded to nearest.  A product waits for the one before it, so with registers to
+                    // spare CHAINS sums go side by side (one row of 131071 tokens, fp16: 102 us with four, 111 with one).
+                    constexpr int CHAINS = NT > 1 ? 1 : D % 64 == 0 ? 4 : 3;
 #pragma unroll
-                for (int x = 0; x < MT; ++x)
+                    for (int c0 = 0; c0 < D / 16; c0 += CHAINS) {
+                        float o[CHAINS][4];
 #pragma unroll
-                    for (int n = 0; n < NT; ++n) {
+                        for (int c = 0; c < CHAINS; ++c) o[c][0] = o[c][1] = o[c][2] = o[c][3] = 0.f;
 #pragma unroll
-                        for (int c = 0; c < D / 16; ++c)
-                            paged_mma(acc[n][c], v[x][c][0], v[x][c][1], v[x][c][2], v[x][c][3], hi[x][n][0], hi[x][n][1], T());
+                        for (int y = 0; y < 3; ++y) {
 #pragma unroll
-                        for (int c = 0; c < D / 16; ++c)
-                            paged_mma(acc[n][c], v[x][c][0], v[x][c][1], v[x][c][2], v[x][c][3], lo[x][n][0], lo[x][n][1], T());
+                            for (int x = 0; x < MT; ++x)
+#pragma unroll
+                                for (int c = 0; c < CHAINS; ++c) paged_mma(o[c], v[x][c0 + c][0], v[x][c0 + c][1], v[x][c0 + c][2], v[x][c0 + c][3], w[y][x][0], w[y][x][1], T());
+                            if (Terms::LIFT != 1.f && y < 2) {
+#pragma unroll
+                                for (int c = 0; c < CHAINS; ++c)
+#pragma unroll
+                                    for (int r = 0; r < 4; ++r) o[c][r] *= 1.f / Terms::LIFT;
+                            }
+                        }
+#pragma unroll
+                        for (int c = 0; c < CHAINS; ++c)
+#pragma unroll
+                            for (int r = 0; r < 4; ++r) acc[n][c0 + c][r] += o[c][r];
                     }
+                }
             });
         __syncwarp();   // the ring has been read
         float* out = reinterpret_cast<float*>(ring);
