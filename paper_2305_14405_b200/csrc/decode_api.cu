@@ -68,8 +68,8 @@ nm_status nm_qk_norm_rope_pwl(nm_ctx* ctx, const nm_qk_rope_desc* d, void* strea
     if (!float_type(d->dtype)) return NM_ERR_UNSUPPORTED;
     if (d->d < 8 || d->d > 256 || d->d % 8) return NM_ERR_SHAPE;
     if (d->rot < 0 || d->rot > d->d || d->rot % (d->pairs ? 8 : 16)) return NM_ERR_SHAPE;
-    const bool norm_q = d->gamma_q && d->heads > 0, norm_k = d->gamma_k && d->kv_heads > 0;
-    if (norm_q || norm_k) {
+    if ((d->gamma_q || d->gamma_k) && (d->rsqrt_slot < 0 || d->rsqrt_slot >= NM_NUM_SLOTS)) return NM_ERR_INVALID_ARG;
+    if (nm_qk_rope_norms(d)) {
         const nm_status s = need_table(ctx, d->rsqrt_slot);
         if (s != NM_OK) return s;
     }

@@ -820,6 +820,8 @@ struct NmDeviceScope {
     }
 };
 nm_status nm_launch_kv_plan(nm_ctx* ctx, const nm_kv_plan_desc* d, cudaStream_t st);
+// whether any head is normed, so that the table is read (a gamma of no heads does not count)
+static inline bool nm_qk_rope_norms(const nm_qk_rope_desc* d) { return (d->gamma_q && d->heads > 0) || (d->gamma_k && d->kv_heads > 0); }
 nm_status nm_launch_qk_rope(nm_ctx* ctx, const nm_qk_rope_desc* d, cudaStream_t st);
 size_t nm_attention_paged_bytes(const nm_attn_paged_desc* d);   // of a checked descriptor
 nm_status nm_launch_attention_paged(nm_ctx* ctx, const nm_attn_paged_desc* d, void* workspace, cudaStream_t st);

@@ -342,7 +342,7 @@ nm_status launch(nm_ctx* ctx, const nm_qk_rope_desc* d, cudaStream_t st)
     a.lanes = lanes;
     a.inv_d = (float)(1.0 / d->d);
     a.d = *d;
-    a.tab = ctx->d_tables + (d->gamma_q || d->gamma_k ? d->rsqrt_slot : 0);
+    a.tab = ctx->d_tables + (nm_qk_rope_norms(d) ? d->rsqrt_slot : 0);
     a.status = ctx->d_status;
     // A unit is up to U groups of a token's heads: fewer where there are so few tokens that the SMs' warps are not all taken, but not so few
     // that some warps get a second unit (700 tokens, 32 + 8 heads of 128, bf16: 10.5 us with 2800 units for 2368 warps, 6.9 with 2100).

@@ -1,0 +1,23 @@
+"""CPU-only checks of the decoding operators' entry points: calls that a launch must never see."""
+import ctypes as C
+
+import pytest
+import torch
+
+import paper_2305_14405_b200 as nm
+from test_decode_host import A, INVALID, NO_TABLE, SHAPE, ctx, lib, rope_desc  # noqa: F401
+
+
+@pytest.mark.parametrize("slot", [-1, 16, 99, -2 ** 31])
+@pytest.mark.parametrize("norm", [{"heads": 0, "gamma_k": None}, {"kv_heads": 0, "gamma_q": None}, {"heads": 0}, {"kv_heads": 0}])
+def test_rope_table_of_no_heads(lib, ctx, norm, slot):  # noqa: F811
+    """A gamma for heads that are not there needs no table, but a number that is no slot is refused all the same."""
+    assert lib.nm_qk_norm_rope_pwl(ctx, C.byref(rope_desc(rsqrt_slot=slot, **norm)), None) == INVALID
+
+
+def test_rope_table_that_is_not_needed(lib, ctx):  # noqa: F811
+    no_launch = 6   # all arguments passed; there is no device
+    for norm in ({"heads": 0, "gamma_k": None}, {"kv_heads": 0, "gamma_q": None}):
+        assert lib.nm_qk_norm_rope_pwl(ctx, C.byref(rope_desc(rsqrt_slot=9, **norm)), None) == no_launch   # slot 9 holds no table
+    assert lib.nm_qk_norm_rope_pwl(ctx, C.byref(rope_desc(rsqrt_slot=9, heads=0)), None) == NO_TABLE
+    assert lib.nm_qk_norm_rope_pwl(ctx, C.byref(rope_desc(rsqrt_slot=99, gamma_q=None, gamma_k=None)), None) == no_launch
