@@ -455,7 +455,8 @@ nm_status nm_encoder_layer_static(nm_ctx* ctx, const nm_encoder_weights* w, cons
  * one new token per sequence.)
  * A cache is num_pages pages of page_size tokens; element (page, token, head, channel) of K and of V is at
  * base[page*stride_page + token*stride_token + head*stride_head + channel].  A slot number is page*page_size + token.
- * Requests, tokens, a request's length, free pages, and M, N, K are at most 2^30 each, otherwise NM_ERR_SHAPE.
+ * Requests, tokens, a request's length, free pages, elements of a token's row, and M, N, K are at most 2^30 each, otherwise
+ * NM_ERR_SHAPE.
  * Page and slot numbers are checked on the device: one that lies outside the cache is never followed.  The kernel then leaves
  * out the access, records NM_ERR_INVALID_ARG in the status word and goes on; what the request or token gets is not meaningful. */
 

@@ -16,10 +16,10 @@ bool float_type(nm_dtype t) { return t == NM_F32 || t == NM_BF16 || t == NM_F16;
 bool aligned4(const void* p) { return ((uintptr_t)p & 3u) == 0; }
 bool rows16(int64_t stride, size_t es) { return (stride * (int64_t)es) % 16 == 0; }
 
-// The distances of a cache's pages, tokens and heads: none negative, 16-byte rows (or a distance that is never used).
-// Counts of requests, tokens, pages and channels: the kernels step through them in 32 bits, some thousands at a time.
+// Counts of requests, tokens and pages, and elements of a token's row: the kernels step through them in 32 bits, some thousands at a time.
 constexpr int64_t DECODE_MAX = 1 << 30;
 
+// The distances of a cache's pages, tokens and heads: none negative, 16-byte rows (or a distance that is never used).
 nm_status check_cache(int32_t num_pages, int32_t page_size, int64_t sp, int64_t st, int64_t sh, size_t es)
 {
     if (num_pages < 1 || page_size < 1 || (int64_t)num_pages * page_size > INT32_MAX) return NM_ERR_SHAPE;
@@ -30,7 +30,7 @@ nm_status check_cache(int32_t num_pages, int32_t page_size, int64_t sp, int64_t 
 nm_status check_attn_paged(const nm_attn_paged_desc* d)
 {
     if (d->B < 0 || d->heads < 1 || d->kv_heads < 1 || d->heads % d->kv_heads || d->max_len < 0) return NM_ERR_SHAPE;
-    if (d->B > DECODE_MAX || d->max_len > DECODE_MAX || (int64_t)d->heads * d->d > INT32_MAX) return NM_ERR_SHAPE;
+    if (d->B > DECODE_MAX || d->max_len > DECODE_MAX || (int64_t)d->heads * d->d > DECODE_MAX) return NM_ERR_SHAPE;
     if ((double)d->B * d->heads * d->max_len > 1e15) return NM_ERR_SHAPE;   // the workspace's size fits 64 bits
     if (!float_type(d->dtype)) return NM_ERR_UNSUPPORTED;
     if (d->d < 8 || d->d > 256 || d->d % 8) return NM_ERR_SHAPE;
@@ -75,7 +75,7 @@ nm_status nm_qk_norm_rope_pwl(nm_ctx* ctx, const nm_qk_rope_desc* d, void* strea
     }
     if (d->T == 0 || (d->heads == 0 && d->kv_heads == 0)) return NM_OK;
     const int64_t row = ((int64_t)d->heads + 2 * (int64_t)d->kv_heads) * d->d;
-    if (row > INT32_MAX) return NM_ERR_SHAPE;
+    if (row > DECODE_MAX) return NM_ERR_SHAPE;
     if (!d->qkv || (d->heads > 0 && !d->q_out)) return NM_ERR_INVALID_ARG;
     if (d->ld_qkv < row || (d->heads > 0 && d->ld_q < (int64_t)d->heads * d->d)) return NM_ERR_SHAPE;
     if (d->k_out && d->ld_k < (int64_t)d->kv_heads * d->d) return NM_ERR_SHAPE;

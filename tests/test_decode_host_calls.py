@@ -5,7 +5,7 @@ import pytest
 import torch
 
 import paper_2305_14405_b200 as nm
-from test_decode_host import A, INVALID, NO_TABLE, SHAPE, ctx, lib, rope_desc  # noqa: F401
+from test_decode_host import A, INVALID, NO_TABLE, SHAPE, attn_desc, ctx, lib, rope_desc  # noqa: F401
 
 
 @pytest.mark.parametrize("slot", [-1, 16, 99, -2 ** 31])
@@ -21,3 +21,12 @@ def test_rope_table_that_is_not_needed(lib, ctx):  # noqa: F811
         assert lib.nm_qk_norm_rope_pwl(ctx, C.byref(rope_desc(rsqrt_slot=9, **norm)), None) == no_launch   # slot 9 holds no table
     assert lib.nm_qk_norm_rope_pwl(ctx, C.byref(rope_desc(rsqrt_slot=9, heads=0)), None) == NO_TABLE
     assert lib.nm_qk_norm_rope_pwl(ctx, C.byref(rope_desc(rsqrt_slot=99, gamma_q=None, gamma_k=None)), None) == no_launch
+
+
+def test_rows_whose_steps_would_not_fit_32_bits(lib, ctx):  # noqa: F811
+    """Threads step through a token's row by some hundreds, and count the heads that fill up its last groups."""
+    wide, heads = 1 << 31, 1 << 24   # 2^30 elements of 64 channels and some more
+    assert lib.nm_qk_norm_rope_pwl(ctx, C.byref(rope_desc(heads=heads, ld_qkv=wide, ld_q=wide)), None) == SHAPE
+    d = attn_desc(heads=heads + 2, ld_q=wide, ld_out=wide)
+    assert lib.nm_attention_pwl_paged(ctx, C.byref(d), A, 1 << 40, None) == SHAPE
+    assert lib.nm_attention_paged_workspace_bytes(C.byref(d)) == 0
