@@ -451,6 +451,9 @@ nm_status nm_encoder_layer_static(nm_ctx* ctx, const nm_encoder_weights* w, cons
 /* ---------------------------------------------------------------- answering token by token
  * A decoder that keeps its keys and values in pages runs, per layer and step,
  *     nm_kv_plan (once per step), nm_linear_pwl[_w4], nm_qk_norm_rope_pwl, nm_attention_pwl_paged, nm_linear_pwl[_w4].
+ * The plan numbers a step's new tokens one after another; a row of every operator is such a token.  The attention, which works by
+ * request, finds a request's row in the plan's token_start (without it, row b is taken to be request b's: a step that adds one token to
+ * every request).
  * (The paper evaluates encoders; these are the operators that the same method, linear operators and PWL tables, needs for
  * one new token per sequence.)
  * A cache is num_pages pages of page_size tokens; element (page, token, head, channel) of K and of V is at
@@ -539,8 +542,14 @@ nm_status nm_qk_norm_rope_pwl(nm_ctx* ctx, const nm_qk_rope_desc* desc, void* st
  * m is the maximum over all of the request's tokens (a PWL exponential is not multiplicative).  A request of length 0 gets
  * zeros.  Token j is at page block_tables[b*ld_tables + j / page_size], place j % page_size; entries and places behind the
  * length are not read.  A length outside [0, max_len] is recorded as NM_ERR_SHAPE in the status word and the request's
- * output left as it was.  max_len (at most max_pages*page_size) is what the launch and the workspace are sized for.
- * Q [B, heads*d], pitch ld_q; out likewise, ld_out.  dtype F32, BF16 or F16 for Q, the caches and out; fp32 scores, sums and
+ * output left as it was.
+ * token_start NULL: Q and out [B, heads*d], row b is request b's.  Else token_start[0..B] as nm_kv_plan leaves it, Q and out
+ * [rows, heads*d]: request b's query and output are row token_start[b+1] - 1, its last new token's; a request without a new token
+ * (token_start[b+1] == token_start[b]) is left out, whatever its length, and rows that are no request's are left as they were.  A
+ * token_start that falls, or leaves [0, rows], is recorded as NM_ERR_INVALID_ARG and the request left out (a row that two requests
+ * then claim is one's or the other's).
+ * max_len (at most max_pages*page_size) is what the launch and the workspace are sized for.
+ * Pitches ld_q and ld_out.  dtype F32, BF16 or F16 for Q, the caches and out; fp32 scores, sums and
  * probabilities (the 16-bit types multiply probabilities into V as three 16-bit terms that add up to the fp32 number; for F16 to 2^-45 at
  * best and up to 65504, and there an |e| below 2^-24 gives NaN with an infinite V).
  * heads a multiple of kv_heads; d a multiple of 8, at most 256.  Pointers 16-byte aligned, strides multiples of 16 bytes.
@@ -562,6 +571,8 @@ typedef struct {
     int32_t exp_slot, recip_slot;
     void* out;
     int64_t ld_out;
+    const int32_t* token_start;
+    int32_t rows;
 } nm_attn_paged_desc;
 
 size_t nm_attention_paged_workspace_bytes(const nm_attn_paged_desc* desc);

@@ -129,7 +129,7 @@ class AttnPagedDesc(C.Structure):
                 ("Q", C.c_void_p), ("ld_q", C.c_int64), ("k_cache", C.c_void_p), ("v_cache", C.c_void_p),
                 ("stride_page", C.c_int64), ("stride_token", C.c_int64), ("stride_head", C.c_int64), ("block_tables", C.c_void_p),
                 ("ld_tables", C.c_int64), ("lengths", C.c_void_p), ("scale", C.c_float), ("exp_slot", C.c_int32),
-                ("recip_slot", C.c_int32), ("out", C.c_void_p), ("ld_out", C.c_int64)]
+                ("recip_slot", C.c_int32), ("out", C.c_void_p), ("ld_out", C.c_int64), ("token_start", C.c_void_p), ("rows", C.c_int32)]
 
 
 class LinearW4Desc(C.Structure):
@@ -531,14 +531,21 @@ class Context:
         _check(self._lib.nm_qk_norm_rope_pwl(self._h, C.byref(desc), self._stream(stream)), "nm_qk_norm_rope_pwl")
 
     @staticmethod
-    def attn_paged_desc(q, k_cache, v_cache, block_tables, lengths, out, max_len=None, scale=None, exp_slot=SLOT_EXP, recip_slot=SLOT_RECIP):
+    def attn_paged_desc(q, k_cache, v_cache, block_tables, lengths, out, max_len=None, scale=None, exp_slot=SLOT_EXP, recip_slot=SLOT_RECIP,
+                        token_start=None):
         """q, out [B, heads, d] (contiguous heads); caches [num_pages, page_size, kv_heads, d]; block_tables int32 [B, max_pages],
-        lengths int32 [B].  max_len: the longest request that the calls have to take (None: what the tables hold)."""
+        lengths int32 [B].  max_len: the longest request that the calls have to take (None: what the tables hold).
+        token_start: the plan's int32 [B + 1]; q, out [tokens, heads, d] then have a row for each of the step's new tokens, and a request's row is its
+        last new token's.  Needed for every step in which some request gets no token, ends, or gets several."""
         torch = _torch()
         a = AttnPagedDesc()
-        B, heads, d = _want("q", q, q.dtype, (None, None, None)).shape
+        rows, heads, d = _want("q", q, q.dtype, (None, None, None)).shape
+        B = rows
+        if token_start is not None:
+            B = block_tables.shape[0] if block_tables.dim() == 2 else 0
+            a.token_start, a.rows = _want("token_start", token_start, torch.int32, (B + 1,)).data_ptr(), rows
         for name, t in (("q", q), ("out", out)):
-            _want(name, t, q.dtype, (B, heads, d))
+            _want(name, t, q.dtype, (rows, heads, d))
             if heads > 1 and t.stride(1) != d:
                 raise ValueError("%s: the heads of a request have to be contiguous" % name)
         a.B, a.heads, a.d, a.dtype, a.kv_heads = B, heads, d, dtype_of(q), k_cache.shape[2] if k_cache.dim() == 4 else 0
@@ -548,12 +555,12 @@ class Context:
         a.max_pages = block_tables.shape[1]
         a.max_len = a.max_pages * a.page_size if max_len is None else int(max_len)
         row = heads * d
-        a.Q, a.ld_q, a.out, a.ld_out = q.data_ptr(), q.stride(0) if B > 1 else row, out.data_ptr(), out.stride(0) if B > 1 else row
+        a.Q, a.ld_q, a.out, a.ld_out = q.data_ptr(), q.stride(0) if rows > 1 else row, out.data_ptr(), out.stride(0) if rows > 1 else row
         a.k_cache, a.v_cache = k_cache.data_ptr(), v_cache.data_ptr()
         a.block_tables, a.ld_tables, a.lengths = block_tables.data_ptr(), _pitch(block_tables) if B else a.max_pages, lengths.data_ptr()
         a.scale = float(scale) if scale is not None else float(d) ** -0.5
         a.exp_slot, a.recip_slot = exp_slot, recip_slot
-        a.tensors = [q, k_cache, v_cache, block_tables, lengths, out]
+        a.tensors = [q, k_cache, v_cache, block_tables, lengths, out, token_start]
         _same_device(a.tensors)
         return a
 

@@ -21,10 +21,10 @@ namespace {
 
 constexpr int PAGED_WARPS = 8, PAGED_THREADS = PAGED_WARPS * 32, PAGED_RING = 8192;   // bytes of a warp's ring
 
-// A unit that begins in a block and goes on (nh = 0: none): its last block, request and query heads, and whether it begins where the
+// A unit that begins in a block and goes on (nh = 0: none): its last block, row of the output and query heads, and whether it begins where the
 // block does (paged_place).
 struct PagedJoin {
-    int c1, b, h0, nh, first_place;
+    int c1, row, h0, nh, first_place;
 };
 
 struct PagedArgs {
@@ -64,15 +64,23 @@ struct PagedExp {
     }
 };
 
-// The length of request b, or -1 where it is outside what the call was made for (recorded; nothing is written then).
-__device__ __forceinline__ int paged_length(const PagedArgs& a, int b)
+// The length of request b and the row of its query and output; row -1 where nothing is read or written for it: it has no new token, or its
+// length or row is outside what the call was made for (*error).
+struct PagedRequest {
+    int len, row;
+};
+__device__ __forceinline__ PagedRequest paged_request(const PagedArgs& a, int b, int* error)
 {
     const int n = a.d.lengths[b];
-    if (n < 0 || n > a.d.max_len) {
-        if (threadIdx.x == 0) atomicExch(a.status, (int)NM_ERR_SHAPE);
-        return -1;
+    int row = b;
+    bool good = true;
+    if (a.d.token_start) {
+        const int start = a.d.token_start[b], end = a.d.token_start[b + 1];
+        good = start >= 0 && end >= start && end <= a.d.rows;
+        row = end > start ? end - 1 : -1;
     }
-    return n;
+    *error = !good ? (int)NM_ERR_INVALID_ARG : row >= 0 && (n < 0 || n > a.d.max_len) ? (int)NM_ERR_SHAPE : 0;
+    return *error || row < 0 ? PagedRequest{0, -1} : PagedRequest{n, row};
 }
 
 // The tokens of one unit that a block works on.
@@ -733,15 +741,18 @@ __global__ void __launch_bounds__(PAGED_THREADS, paged_blocks(Core::RING)) paged
     const PagedUnit u = paged_unit<Core>(a, blockIdx.x / ctas);
     nm_grid_launch_dependents();
     nm_grid_dependency_wait();
-    const int len = paged_length(a, u.b);
-    if (len < 0) return;   // the whole cluster
+    int error;
+    const PagedRequest request = paged_request(a, u.b, &error);
+    if (error && threadIdx.x == 0) atomicExch(a.status, error);
+    if (request.row < 0) return;   // the whole cluster
+    const int len = request.len;
     const int per = ((len + (int)ctas - 1) / (int)ctas + 31) / 32 * 32, first = min(len, rank * per);
     const PagedTokens tok = {a.d.block_tables + (int64_t)u.b * a.d.ld_tables, first, min(len - first, per)};
     const int pitch = paged_pitch(a.span), warp = threadIdx.x >> 5;
     unsigned char* ring = paged_smem + warp * Core::RING;
     int64_t* offsets = reinterpret_cast<int64_t*>(paged_smem + PAGED_WARPS * Core::RING) + warp * 64;
     float* sc = reinterpret_cast<float*>(paged_smem + PAGED_WARPS * Core::RING + PAGED_OFFSETS);
-    Core::scores(a, (const T*)a.d.Q + (int64_t)u.b * a.d.ld_q + (int64_t)u.h0 * a.d.d, u.nh, (const T*)a.d.k_cache + (int64_t)u.kv * a.d.stride_head,
+    Core::scores(a, (const T*)a.d.Q + (int64_t)request.row * a.d.ld_q + (int64_t)u.h0 * a.d.d, u.nh, (const T*)a.d.k_cache + (int64_t)u.kv * a.d.stride_head,
                  tok, ring, offsets, s_max[warp], [&](int h, int i, float s) { sc[h * pitch + i] = s; });
     Core::values(
         a, u.nh, (const T*)a.d.v_cache + (int64_t)u.kv * a.d.stride_head, tok, exp, ring, offsets, s_sum[warp],
@@ -795,7 +806,7 @@ __global__ void __launch_bounds__(PAGED_THREADS, paged_blocks(Core::RING)) paged
             o += po;
             s += ps;
         }
-        ((T*)a.d.out)[(int64_t)u.b * a.d.ld_out + (int64_t)(u.h0 + h) * a.d.d + c] = NmType<T>::from_f(len ? o * paged_table(a.recip_tab, s) : 0.f);
+        ((T*)a.d.out)[(int64_t)request.row * a.d.ld_out + (int64_t)(u.h0 + h) * a.d.d + c] = NmType<T>::from_f(len ? o * paged_table(a.recip_tab, s) : 0.f);
     }
     if (ctas > 1) nm_cluster_sync();   // no block leaves while another reads its shared memory
 }
@@ -805,18 +816,26 @@ __global__ void __launch_bounds__(PAGED_THREADS, paged_blocks(Core::RING)) paged
 // unit covers the block's first position, its tail segment otherwise, so a block has room for the sums of two.
 struct PagedShare {
     int64_t share, pos, end, row0;   // the block's positions still to do; where the current request's first unit begins
-    int b, len;                      // the current request
+    int b, len, row;                 // the current request
 };
 __device__ __forceinline__ int paged_len32(int len) { return (len + 31) & ~31; }
 
 // Positions of a unit: some without a token, for what a segment costs next to its tokens, then its tokens as whole 32s.
 __device__ __forceinline__ int64_t paged_width(const PagedArgs& a, int len) { return len ? (int64_t)a.lead + paged_len32(len) : 0; }
 
-// Length of request b for the shares: 0 where it is outside what the call was made for.
+// Length of request b for the shares: 0 where nothing is done for it.
 __device__ __forceinline__ int paged_length_or_0(const PagedArgs& a, int b)
 {
-    const int n = a.d.lengths[b];
-    return n < 0 || n > a.d.max_len ? 0 : n;
+    int error;
+    return paged_request(a, b, &error).len;
+}
+__device__ __forceinline__ void paged_go_to(const PagedArgs& a, PagedShare& s, int b)
+{
+    int error;
+    const PagedRequest r = paged_request(a, b, &error);
+    s.b = b;
+    s.len = r.len;
+    s.row = r.row;
 }
 
 // The block's share: two passes over the lengths, 256 requests at a time.
@@ -841,7 +860,7 @@ __device__ __forceinline__ PagedShare paged_share(const PagedArgs& a, int units)
     if (s.share < a.span) s.share = a.span;
     s.pos = (int64_t)blockIdx.x * s.share;
     s.end = s.pos + s.share < total ? s.pos + s.share : total;
-    s.b = s.len = 0;
+    s.b = s.len = s.row = 0;
     s.row0 = 0;
     if (s.pos >= s.end) return s;
     int64_t before = 0;   // of the requests of earlier turns
@@ -870,13 +889,12 @@ __device__ __forceinline__ PagedShare paged_share(const PagedArgs& a, int units)
         if (before > s.pos) break;
     }
     __syncthreads();
-    s.b = s_b;
     s.row0 = s_row0;
-    s.len = paged_length_or_0(a, s.b);
+    paged_go_to(a, s, s_b);
     return s;
 }
 struct PagedSegment {
-    int b, unit, first, count;   // request, unit of it, tokens
+    int b, row, unit, first, count;   // request, its row, unit of it, tokens
     int64_t from;                // the unit's first position
     bool whole;                  // the unit lies in this block alone
 };
@@ -887,11 +905,12 @@ __device__ __forceinline__ bool paged_next(const PagedArgs& a, PagedShare& s, in
     int64_t width = paged_width(a, s.len);
     while (s.pos >= s.row0 + width * units) {   // the next request that has tokens
         s.row0 += width * units;
-        s.len = paged_length_or_0(a, ++s.b);
+        paged_go_to(a, s, s.b + 1);
         width = paged_width(a, s.len);
     }
     const int len32 = paged_len32(s.len);
     g->b = s.b;
+    g->row = s.row;
     g->unit = (int)((s.pos - s.row0) / width);
     g->from = s.row0 + g->unit * width + a.lead;
     if (s.pos < g->from) s.pos = g->from;
@@ -927,7 +946,7 @@ __global__ void __launch_bounds__(PAGED_THREADS, paged_blocks(Core::RING)) paged
         const PagedUnit u = paged_unit<Core>(a, (int64_t)g.b * units + g.unit);
         const PagedTokens tok = {a.d.block_tables + (int64_t)u.b * a.d.ld_tables, g.first, g.count};
         float* sc = a.scores + ((int64_t)u.b * a.d.heads + u.h0) * a.row + g.first;
-        Core::scores(a, (const T*)a.d.Q + (int64_t)u.b * a.d.ld_q + (int64_t)u.h0 * a.d.d, u.nh, (const T*)a.d.k_cache + (int64_t)u.kv * a.d.stride_head,
+        Core::scores(a, (const T*)a.d.Q + (int64_t)g.row * a.d.ld_q + (int64_t)u.h0 * a.d.d, u.nh, (const T*)a.d.k_cache + (int64_t)u.kv * a.d.stride_head,
                      tok, ring, offsets, s_max[warp], [&](int h, int i, float s) {
                          if (h < u.nh) sc[h * a.row + i] = s;
                      });
@@ -1004,18 +1023,18 @@ __global__ void __launch_bounds__(PAGED_THREADS, paged_blocks(Core::RING)) paged
     int64_t* offsets = reinterpret_cast<int64_t*>(paged_smem + PAGED_WARPS * Core::RING) + warp * 64;
     const float* out = reinterpret_cast<const float*>(paged_smem);
     nm_grid_launch_dependents();
-    // Only the scores come from the launch before, which has let this one start once everything before it was complete: lengths,
+    // Only the scores come from the launch before, which has let this one start once everything before it was complete: lengths, rows,
     // tables and the first values are read before it is done.
     PagedShare share = paged_share(a, units);
     bool waited = false;
     for (int b = blockIdx.x; b < a.d.B; b += gridDim.x) {
-        const int n = a.d.lengths[b];
-        if (n < 0 || n > a.d.max_len) {
-            if (threadIdx.x == 0) atomicExch(a.status, (int)NM_ERR_SHAPE);
-        } else if (n == 0) {
+        int error;
+        const PagedRequest r = paged_request(a, b, &error);
+        if (error && threadIdx.x == 0) atomicExch(a.status, error);
+        if (r.row >= 0 && r.len == 0) {
             if (!waited) nm_grid_dependency_wait();   // nothing is written before
             waited = true;
-            for (int x = threadIdx.x; x < a.d.heads * a.d.d; x += PAGED_THREADS) ((T*)a.d.out)[(int64_t)b * a.d.ld_out + x] = NmType<T>::from_f(0.f);
+            for (int x = threadIdx.x; x < a.d.heads * a.d.d; x += PAGED_THREADS) ((T*)a.d.out)[(int64_t)r.row * a.d.ld_out + x] = NmType<T>::from_f(0.f);
         }
     }
     PagedSegment g;
@@ -1048,7 +1067,7 @@ __global__ void __launch_bounds__(PAGED_THREADS, paged_blocks(Core::RING)) paged
             },
             [&](int h, int i) { return Core::read(sc + h * a.row + i); });
         __syncthreads();
-        T* result = (T*)a.d.out + (int64_t)u.b * a.d.ld_out + (int64_t)u.h0 * a.d.d;
+        T* result = (T*)a.d.out + (int64_t)g.row * a.d.ld_out + (int64_t)u.h0 * a.d.d;
         float* part = a.parts + paged_place(g.from, share.share, blockIdx.x) * paged_part_floats(Core::HEADS, a.d.d);
         for (int x = threadIdx.x; x < u.nh * Core::D; x += PAGED_THREADS) {
             const int h = x / Core::D, c = x - h * Core::D;
@@ -1067,7 +1086,7 @@ __global__ void __launch_bounds__(PAGED_THREADS, paged_blocks(Core::RING)) paged
         }
         if (!g.whole) {   // the unit's last block adds up what all of them left, in their order
             if (a.joins) {
-                if (g.first == 0 && threadIdx.x == 0) a.joins[c0] = PagedJoin{(int)c1, u.b, u.h0, u.nh, g.from == c0 * share.share};
+                if (g.first == 0 && threadIdx.x == 0) a.joins[c0] = PagedJoin{(int)c1, g.row, u.h0, u.nh, g.from == c0 * share.share};
                 __syncthreads();   // the ring and the sums have been read
                 continue;
             }
@@ -1141,7 +1160,7 @@ __global__ void __launch_bounds__(JOIN_THREADS) paged_join_kernel(const PagedArg
     }
     const float2 kb = s_recip[nm_pwl_index(s, inv_h, off, nm1)];
     const float r = __fmaf_rn(kb.x, s, kb.y);
-    T* result = (T*)a.d.out + (int64_t)j.b * a.d.ld_out + (int64_t)(j.h0 + h) * a.d.d + x * 4;
+    T* result = (T*)a.d.out + (int64_t)j.row * a.d.ld_out + (int64_t)(j.h0 + h) * a.d.d + x * 4;
     result[0] = NmType<T>::from_f(o.x * r);
     result[1] = NmType<T>::from_f(o.y * r);
     result[2] = NmType<T>::from_f(o.z * r);

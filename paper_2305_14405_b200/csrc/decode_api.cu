@@ -111,13 +111,14 @@ nm_status nm_attention_pwl_paged(nm_ctx* ctx, const nm_attn_paged_desc* d, void*
     s = need_table(ctx, d->recip_slot);
     if (s != NM_OK) return s;
     if (!(d->scale > 0.0f) || !isfinite(d->scale)) return NM_ERR_INVALID_ARG;
-    if (d->B == 0) return NM_OK;
+    if (d->token_start && (d->rows < 0 || d->rows > DECODE_MAX)) return NM_ERR_SHAPE;
+    if (d->B == 0 || (d->token_start && d->rows == 0)) return NM_OK;
     if (!d->Q || !d->k_cache || !d->v_cache || !d->lengths || !d->out || (d->max_pages > 0 && !d->block_tables)) return NM_ERR_INVALID_ARG;
     const size_t es = nm_dtype_size(d->dtype);
     const int64_t row = (int64_t)d->heads * d->d;
     if (d->ld_q < row || d->ld_out < row || d->ld_tables < d->max_pages) return NM_ERR_SHAPE;
     if (!nm_aligned16(d->Q) || !nm_aligned16(d->k_cache) || !nm_aligned16(d->v_cache) || !nm_aligned16(d->out) ||
-        !aligned4(d->block_tables) || !aligned4(d->lengths) || !rows16(d->ld_q, es) || !rows16(d->ld_out, es))
+        !aligned4(d->block_tables) || !aligned4(d->lengths) || !aligned4(d->token_start) || !rows16(d->ld_q, es) || !rows16(d->ld_out, es))
         return NM_ERR_ALIGNMENT;
     const size_t need = nm_attention_paged_bytes(d);
     if (need > 0 && (!workspace || ws_bytes < need)) return NM_ERR_WORKSPACE;

@@ -5,7 +5,7 @@ import pytest
 import torch
 
 import paper_2305_14405_b200 as nm
-from test_decode_host import A, INVALID, NO_TABLE, SHAPE, attn_desc, ctx, lib, rope_desc  # noqa: F401
+from test_decode_host import A, ALIGN, INVALID, NO_TABLE, SHAPE, attn_desc, ctx, lib, rope_desc  # noqa: F401
 
 
 @pytest.mark.parametrize("slot", [-1, 16, 99, -2 ** 31])
@@ -30,3 +30,27 @@ def test_rows_whose_steps_would_not_fit_32_bits(lib, ctx):  # noqa: F811
     d = attn_desc(heads=heads + 2, ld_q=wide, ld_out=wide)
     assert lib.nm_attention_pwl_paged(ctx, C.byref(d), A, 1 << 40, None) == SHAPE
     assert lib.nm_attention_paged_workspace_bytes(C.byref(d)) == 0
+
+
+@pytest.mark.parametrize("change,status", [({"rows": -1}, SHAPE), ({"rows": (1 << 30) + 1}, SHAPE), ({"token_start": A + 2}, ALIGN), ({"rows": 0, "Q": None}, 0),
+                                           ({"rows": 3, "Q": None}, INVALID), ({"rows": 3, "max_len": 65}, SHAPE)])
+def test_attention_with_rows_of_a_plan(lib, ctx, change, status):  # noqa: F811
+    d = attn_desc(**dict({"token_start": A, "rows": 5}, **change))
+    assert lib.nm_attention_pwl_paged(ctx, C.byref(d), A, 1 << 30, None) == status
+
+
+def test_binding_of_the_rows_of_a_plan(lib):  # noqa: F811
+    if torch.cuda.is_available():
+        pytest.skip("a machine without a device")
+    i = torch.int32
+    z = lambda *shape, dtype=torch.bfloat16: torch.zeros(shape, dtype=dtype)  # noqa: E731
+    cache = z(9, 16, 2, 64)
+    good = dict(q=z(11, 8, 64), k_cache=cache, v_cache=cache, block_tables=z(2, 4, dtype=i), lengths=z(2, dtype=i), out=z(11, 8, 64), token_start=z(3, dtype=i))
+    d = nm.Context.attn_paged_desc(**good)
+    assert (d.B, d.rows, d.ld_q, d.ld_out) == (2, 11, 512, 512) and d.token_start
+    d = nm.Context.attn_paged_desc(**dict(good, q=z(1, 8, 64), out=z(1, 8, 64)))
+    assert (d.B, d.rows, d.ld_q) == (2, 1, 512)
+    for bad in ({"token_start": z(2, dtype=i)}, {"token_start": z(12, dtype=i)}, {"token_start": z(3, dtype=torch.int64)}, {"lengths": z(11, dtype=i)},
+                {"out": z(2, 8, 64)}, {"block_tables": z(4, dtype=i)}, {"token_start": None}):
+        with pytest.raises(ValueError):
+            nm.Context.attn_paged_desc(**dict(good, **bad))

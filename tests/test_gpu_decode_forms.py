@@ -5,7 +5,7 @@ import torch
 
 import decode_ref as ref
 from decode_ref import TYPES, check, f64
-from test_gpu_decode import cache_views, check_attention, ctx, gen_of, i32, make_cache, randn  # noqa: F401
+from test_gpu_decode import Layer, check_attention, ctx, gen_of, i32, make_cache, randn  # noqa: F401
 
 pytestmark = pytest.mark.gpu
 
@@ -21,3 +21,124 @@ def test_rope_gamma_of_no_heads(ctx, dtype, hq, hk):  # noqa: F811
     ctx.qk_norm_rope_pwl(ctx.qk_rope_desc(qkv, hq, hk, d, q, gamma_q=None if hq else g, gamma_k=None if hk else g, k_out=k, rsqrt_slot=15))
     ctx.check_device_status()
     assert torch.equal(q, qkv[:, :hq * d]) and torch.equal(k, qkv[:, hq * d:(hq + hk) * d])
+
+
+# ---------------------------------------------------------------- the rows of a plan
+
+
+@pytest.mark.parametrize("dtype,hq,hk,d", [("bf16", 8, 2, 64), ("f16", 4, 1, 128), ("f32", 6, 2, 64), ("bf16", 3, 3, 40)])
+@pytest.mark.parametrize("max_len,B", [(300, 7), (20000, 7), (20000, 2)])   # one launch, shares of tokens, a third launch where units are few
+def test_attention_finds_its_rows_in_a_plan(ctx, dtype, hq, hk, d, max_len, B):  # noqa: F811
+    """Requests with one new token, several, or none (in use, over, never there): each query and output at its last new token's row; nothing
+    is read or written for a request without one."""
+    td, gen = TYPES[dtype], gen_of(B + d)
+    lens = [129, 300, 40, 0, 17, 250, 64][:B]
+    new = [1, 3, 0, 0, 5, 0, 2][:B] if B > 2 else [0, 2]
+    start = np.concatenate([[0], np.cumsum(new)])
+    rows = int(start[-1]) + 4
+    kc, vc, tables, k, v = make_cache(gen, td, lens, 32, hk, d, "token")
+    wide = torch.full((B, 700), -5, dtype=torch.int32, device="cuda")
+    wide[:, :tables.shape[1]] = tables
+    lengths = i32(lens)
+    for b in range(B):
+        if new[b] == 0:
+            wide[b], lengths[b] = -7, [max_len, max_len + 1, -3][b % 3]
+    q = torch.full((rows, hq + 1, d), float("nan"), dtype=td, device="cuda")[:, :hq]
+    last = [int(start[b + 1]) - 1 for b in range(B) if new[b]]
+    q[last] = randn(gen, len(last), hq, d).to(td)
+    raw = torch.full((rows, hq * d + 8), 5.0, dtype=td, device="cuda")
+    out = raw[:, :hq * d].view(rows, hq, d)
+    desc = ctx.attn_paged_desc(q, kc, vc, wide, lengths, out, max_len=max_len, token_start=i32(start.tolist()))
+    ctx.attention_pwl_paged(desc, torch.full((ctx.attention_paged_workspace_bytes(desc),), 255, dtype=torch.uint8, device="cuda"))
+    ctx.check_device_status()
+    for b in range(B):
+        if new[b]:
+            at = slice(int(start[b + 1]) - 1, int(start[b + 1]))
+            check_attention(ctx, q[at], [k[b]], [v[b]], out[at], [lens[b]], hq, hk, d, td)
+    rest = torch.ones(rows, dtype=torch.bool, device="cuda")
+    rest[last] = False
+    assert (out[rest] == 5).all() and (raw[:, hq * d:] == 5).all()
+
+
+@pytest.mark.parametrize("max_len", [300, 20000])
+def test_attention_refuses_rows_that_are_none(ctx, max_len):  # noqa: F811
+    hq, hk, d, td, lens, rows = 4, 2, 64, torch.bfloat16, [30, 70, 0, 20], 4
+    gen = gen_of(12)
+    kc, vc, tables, k, v = make_cache(gen, td, lens, 32, hk, d, "token")
+    wide = torch.full((4, 700), -5, dtype=torch.int32, device="cuda")
+    wide[:, :tables.shape[1]] = tables
+    q = randn(gen, rows, hq, d).to(td)
+    # (start, requests left out, status)
+    for start, left_out, status in (([0, 1, 2, 3, 4], [], 0), ([0, 1, 5, 5, 5], [1, 2, 3], 1), ([0, 1, 0, 2, 3], [1], 1), ([0, 1, -1, 3, 4], [1, 2], 1),
+                                    ([-2, -1, 2, 3, 4], [0, 1], 1), ([0, 0, 0, 0, 0], [0, 1, 2, 3], 0), ([0, 1, 2 ** 31 - 1, -2 ** 31, 4], [1, 2, 3], 1)):
+        out = torch.full_like(q, 5.0)
+        desc = ctx.attn_paged_desc(q, kc, vc, wide, i32(lens), out, max_len=max_len, token_start=i32(start))
+        ctx.attention_pwl_paged(desc, torch.empty(ctx.attention_paged_workspace_bytes(desc), dtype=torch.uint8, device="cuda"))
+        assert ctx.poll_status() == status, start
+        done = [b for b in range(4) if b not in left_out and start[b + 1] > start[b]]
+        for b in done:
+            r = start[b + 1] - 1
+            check_attention(ctx, q[r:r + 1], [k[b]], [v[b]], out[r:r + 1], [lens[b]], hq, hk, d, td)
+        rest = [r for r in range(rows) if r not in [start[b + 1] - 1 for b in done]]
+        assert (out[rest] == 5).all(), start
+
+
+class PackedLayer(Layer):
+    """A layer whose rows are the step's new tokens, however many each request has."""
+
+    def __init__(self, nm, ctx, seed, B, hq, hk, d, td, max_tokens=64):  # noqa: F811
+        super().__init__(nm, ctx, seed, B, hq, hk, d, td, max_tokens=max_tokens)
+        self.a, self.y = (torch.zeros((max_tokens, self.H), dtype=td, device="cuda") for _ in range(2))
+        self.attn = ctx.attn_paged_desc(self.q.view(max_tokens, hq, d), self.kc, self.vc, self.tables, self.lengths, self.a.view(max_tokens, hq, d),
+                                        token_start=self.start)
+        self.ws = torch.empty(ctx.attention_paged_workspace_bytes(self.attn), dtype=torch.uint8, device="cuda")
+        self.out = ctx.linear_w4_desc(self.a, *self.wo, self.y, residual=self.x)
+
+
+@pytest.mark.parametrize("dtype,hq,hk,d", [("bf16", 4, 2, 64), ("f16", 8, 1, 128), ("f32", 2, 2, 64)])
+def test_decoding_steps_in_which_requests_idle_end_and_join(nm, ctx, dtype, hq, hk, d):  # noqa: F811
+    """Plan, projection, rotation, attention, projection, eager and replayed, over steps of every kind; after each step every request's
+    attention is that of its own query, and what the step did not touch is as it was."""
+    td, B = TYPES[dtype], 6
+    eager, graphed = (PackedLayer(nm, ctx, 9, B, hq, hk, d, td) for _ in range(2))
+    for layer in (eager, graphed):
+        layer.new.copy_(i32([5, 16, 0, 20, 1, 0]))
+        layer.x.copy_(randn(gen_of(50), *layer.x.shape))
+        layer.step()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        graphed.step()
+    steps = [[1, 1, 1, 1, 1, 1], [1, 0, 1, 1, 0, 1], [1, -1, 1, 1, 1, 1], [1, 9, 0, -1, 1, 1], [0, 0, 0, 0, 0, 0], [-1, 1, 1, 4, -1, 1], [30, 1, -1, 1, 20, 0],
+             [1, 1, 0, 1, 1, 1], [60, 1, 1, 1, 1, 1]]
+    for n, new in enumerate(steps):
+        before = eager.a.clone()
+        for layer in (eager, graphed):
+            layer.new.copy_(i32(new))
+            layer.x.copy_(randn(gen_of(100 + n), *layer.x.shape))
+        eager.step()
+        graph.replay()
+        torch.cuda.synchronize()
+        status = 2 if sum(max(x, 0) for x in new) > 64 else 0     # the last step has more tokens than rows: it is left out whole
+        assert ctx.poll_status() == status
+        for s, t in zip(eager.state(), graphed.state()):
+            assert torch.equal(s, t), n
+        start, lens, T = eager.start.tolist(), eager.lengths.tolist(), eager.q.shape[0]
+        touched = []
+        for b in range(B):
+            if status or new[b] <= 0:
+                assert start[b + 1] == start[b]
+                continue
+            r = start[b + 1] - 1
+            touched.append(r)
+            j = torch.arange(lens[b], device="cuda")
+            row = eager.tables[b].long()[j // eager.page]
+            assert int(eager.positions[r]) == lens[b] - 1
+            check_attention(ctx, eager.q.view(T, hq, d)[r:r + 1], [eager.kc[row, j % eager.page]], [eager.vc[row, j % eager.page]],
+                            eager.a.view(T, hq, d)[r:r + 1], [lens[b]], hq, hk, d, td)
+        rest = [r for r in range(T) if r not in touched]
+        assert torch.equal(eager.a[rest], before[rest]), n
+        y, dy = ref.linear_w4(f64(eager.a), eager.wo[0].cpu().numpy(), f64(eager.wo[1]), None, f64(eager.x), None)
+        check(eager.y, y, dy, td, "output")
