@@ -549,6 +549,11 @@ nm_status nm_qk_norm_rope_pwl(nm_ctx* ctx, const nm_qk_rope_desc* desc, void* st
  * token_start that falls, or leaves [0, rows], is recorded as NM_ERR_INVALID_ARG and the request left out (a row that two requests
  * then claim is one's or the other's).
  * max_len (at most max_pages*page_size) is what the launch and the workspace are sized for.
+ * recip_pow2 = 0: the sum goes through the reciprocal's table as it is.  A table of equal segments for lengths up to 8192 is no reciprocal
+ * for the short requests of the batch: 256 segments from 32 to 8193 make the weights of 1 / 16 / 100 / 1000 tokens add up to
+ * 0.05 / 0.20 / 0.55 / 1.05, from 1 to 8193 to 1.0 / 3.9 / 7.9 / 1.2 (scores of unit variance).  recip_pow2 = 1: with sum = m * 2^p and
+ * 1 <= m < 2, PWL_recip(m) * 2^-p, so that a table over [1, 2] serves every length (256 segments: the weights add up to 1 within 4e-6); a sum
+ * that is not positive, normal and finite goes through the table as it is.
  * Pitches ld_q and ld_out.  dtype F32, BF16 or F16 for Q, the caches and out; fp32 scores, sums and
  * probabilities (the 16-bit types multiply probabilities into V as three 16-bit terms that add up to the fp32 number; for F16 to 2^-45 at
  * best and up to 65504, and there an |e| below 2^-24 gives NaN with an infinite V).
@@ -572,7 +577,7 @@ typedef struct {
     void* out;
     int64_t ld_out;
     const int32_t* token_start;
-    int32_t rows;
+    int32_t rows, recip_pow2;
 } nm_attn_paged_desc;
 
 size_t nm_attention_paged_workspace_bytes(const nm_attn_paged_desc* desc);

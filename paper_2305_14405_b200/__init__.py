@@ -129,7 +129,8 @@ class AttnPagedDesc(C.Structure):
                 ("Q", C.c_void_p), ("ld_q", C.c_int64), ("k_cache", C.c_void_p), ("v_cache", C.c_void_p),
                 ("stride_page", C.c_int64), ("stride_token", C.c_int64), ("stride_head", C.c_int64), ("block_tables", C.c_void_p),
                 ("ld_tables", C.c_int64), ("lengths", C.c_void_p), ("scale", C.c_float), ("exp_slot", C.c_int32),
-                ("recip_slot", C.c_int32), ("out", C.c_void_p), ("ld_out", C.c_int64), ("token_start", C.c_void_p), ("rows", C.c_int32)]
+                ("recip_slot", C.c_int32), ("out", C.c_void_p), ("ld_out", C.c_int64), ("token_start", C.c_void_p), ("rows", C.c_int32),
+                ("recip_pow2", C.c_int32)]
 
 
 class LinearW4Desc(C.Structure):
@@ -532,11 +533,13 @@ class Context:
 
     @staticmethod
     def attn_paged_desc(q, k_cache, v_cache, block_tables, lengths, out, max_len=None, scale=None, exp_slot=SLOT_EXP, recip_slot=SLOT_RECIP,
-                        token_start=None):
+                        token_start=None, recip_pow2=False):
         """q, out [B, heads, d] (contiguous heads); caches [num_pages, page_size, kv_heads, d]; block_tables int32 [B, max_pages],
         lengths int32 [B].  max_len: the longest request that the calls have to take (None: what the tables hold).
         token_start: the plan's int32 [B + 1]; q, out [tokens, heads, d] then have a row for each of the step's new tokens, and a request's row is its
-        last new token's.  Needed for every step in which some request gets no token, ends, or gets several."""
+        last new token's.  Needed for every step in which some request gets no token, ends, or gets several.
+        recip_pow2: the reciprocal's table is over [1, 2] and takes the mantissas of the sums; a table over the sums themselves serves
+        requests of similar lengths only."""
         torch = _torch()
         a = AttnPagedDesc()
         rows, heads, d = _want("q", q, q.dtype, (None, None, None)).shape
@@ -559,7 +562,7 @@ class Context:
         a.k_cache, a.v_cache = k_cache.data_ptr(), v_cache.data_ptr()
         a.block_tables, a.ld_tables, a.lengths = block_tables.data_ptr(), _pitch(block_tables) if B else a.max_pages, lengths.data_ptr()
         a.scale = float(scale) if scale is not None else float(d) ** -0.5
-        a.exp_slot, a.recip_slot = exp_slot, recip_slot
+        a.exp_slot, a.recip_slot, a.recip_pow2 = exp_slot, recip_slot, 1 if recip_pow2 else 0
         a.tensors = [q, k_cache, v_cache, block_tables, lengths, out, token_start]
         _same_device(a.tensors)
         return a

@@ -49,6 +49,19 @@ __device__ __forceinline__ float paged_table(const NmTable* t, float x)
     return __fmaf_rn(kb.x, x, kb.y);
 }
 
+// The reciprocal of a row's sum.  Equal segments over all sums from 1 to a long row's length would be far too wide for short rows; with
+// recip_pow2 the table sees the sum's mantissa, in [1, 2), and the power of two is undone exactly.
+template <typename Table> __device__ __forceinline__ float paged_recip(const PagedArgs& a, float s, Table table)
+{
+    const uint32_t bits = __float_as_uint(s);
+    if (!a.d.recip_pow2 || bits - 0x00800000u >= 0x7f000000u) return table(s);   // (zero, subnormal, negative and not finite as they are)
+    return scalbnf(table(__uint_as_float((bits & 0x007fffffu) | 0x3f800000u)), 127 - (int)(bits >> 23));
+}
+__device__ __forceinline__ float paged_recip(const PagedArgs& a, float s)
+{
+    return paged_recip(a, s, [&](float x) { return paged_table(a.recip_tab, x); });
+}
+
 // The exponential's table in shared memory.  floor(u) is taken by adding 1.5 * 2^23 with rounding down, which leaves it in the low bits
 // (0 <= u < 2^22), and the entry's address is formed from those.
 struct PagedExp {
@@ -806,7 +819,7 @@ __global__ void __launch_bounds__(PAGED_THREADS, paged_blocks(Core::RING)) paged
             o += po;
             s += ps;
         }
-        ((T*)a.d.out)[(int64_t)request.row * a.d.ld_out + (int64_t)(u.h0 + h) * a.d.d + c] = NmType<T>::from_f(len ? o * paged_table(a.recip_tab, s) : 0.f);
+        ((T*)a.d.out)[(int64_t)request.row * a.d.ld_out + (int64_t)(u.h0 + h) * a.d.d + c] = NmType<T>::from_f(len ? o * paged_recip(a, s) : 0.f);
     }
     if (ctas > 1) nm_cluster_sync();   // no block leaves while another reads its shared memory
 }
@@ -1002,7 +1015,7 @@ __device__ __forceinline__ void paged_join(const PagedArgs& a, int nh, int64_t f
             o.w += v.w;
             s += s_sum[g * items + x];
         }
-        const float r = paged_table(a.recip_tab, s);
+        const float r = paged_recip(a, s);
         result[x * 4] = NmType<T>::from_f(o.x * r);
         result[x * 4 + 1] = NmType<T>::from_f(o.y * r);
         result[x * 4 + 2] = NmType<T>::from_f(o.z * r);
@@ -1078,7 +1091,7 @@ __global__ void __launch_bounds__(PAGED_THREADS, paged_blocks(Core::RING)) paged
                 s += s_sum[w][h];
             }
             if (g.whole) {
-                result[h * a.d.d + c] = NmType<T>::from_f(o * paged_table(a.recip_tab, s));
+                result[h * a.d.d + c] = NmType<T>::from_f(o * paged_recip(a, s));
             } else {
                 part[h * a.d.d + c] = o;
                 if (c == 0) part[Core::HEADS * a.d.d + h] = s;
@@ -1158,8 +1171,10 @@ __global__ void __launch_bounds__(JOIN_THREADS) paged_join_kernel(const PagedArg
         o.w += v.w;
         s += s_sum[g * d4 + x];
     }
-    const float2 kb = s_recip[nm_pwl_index(s, inv_h, off, nm1)];
-    const float r = __fmaf_rn(kb.x, s, kb.y);
+    const float r = paged_recip(a, s, [&](float x) {
+        const float2 kb = s_recip[nm_pwl_index(x, inv_h, off, nm1)];
+        return __fmaf_rn(kb.x, x, kb.y);
+    });
     T* result = (T*)a.d.out + (int64_t)j.row * a.d.ld_out + (int64_t)(j.h0 + h) * a.d.d + x * 4;
     result[0] = NmType<T>::from_f(o.x * r);
     result[1] = NmType<T>::from_f(o.y * r);

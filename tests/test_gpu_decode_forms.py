@@ -142,3 +142,75 @@ def test_decoding_steps_in_which_requests_idle_end_and_join(nm, ctx, dtype, hq, 
         assert torch.equal(eager.a[rest], before[rest]), n
         y, dy = ref.linear_w4(f64(eager.a), eager.wo[0].cpu().numpy(), f64(eager.wo[1]), None, f64(eager.x), None)
         check(eager.y, y, dy, td, "output")
+
+
+# ---------------------------------------------------------------- a reciprocal for rows of every length
+
+
+RECIP_1_2 = 12   # a slot of its own: the other tests' tables stay
+
+
+class Pow2:
+    """A table over [1, 2] applied to mantissas: the lines of both ends meet at powers of two, up to their rounding."""
+
+    def __init__(self, tab):
+        self.tab = tab
+
+    def __call__(self, x, err=0.0):
+        p = 2.0 ** -np.floor(np.log2(x))
+        r, dr = self.tab(x * p, err * p)
+        return r * p, (dr + 8 * ref.U) * p
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("hq,d", [(1, 64), (12, 64), (4, 40), (2, 128)])
+@pytest.mark.parametrize("max_len,lens", [(600, [1, 3, 16, 100, 600, 0, 2]), (9000, [1, 16, 9000, 4097, 100]), (20000, [20000, 1]), (20000, [1, 30, 999, 7, 0, 2048])])
+def test_attention_is_a_softmax_for_every_length(nm, ctx, dtype, hq, d, max_len, lens):  # noqa: F811
+    """One reciprocal table on [1, 2] for all rows of a call, with recip_pow2."""
+    ctx.load_function_table(RECIP_1_2, nm.FUNC_RECIP, 256, 1.0, 2.0)
+    tab = Pow2(ref.Table(nm.FUNC_RECIP, 256, 1.0, 2.0))
+    td, gen, B = TYPES[dtype], gen_of(len(lens) + d), len(lens)
+    kc, vc, tables, k, v = make_cache(gen, td, lens, 32, 1, d, "token")
+    wide = torch.full((B, -(-max_len // 32)), -5, dtype=torch.int32, device="cuda")
+    width = min(wide.shape[1], tables.shape[1])
+    wide[:, :width] = tables[:, :width]
+    q = randn(gen, B, hq, d).to(td)
+    out = torch.full_like(q, 5.0)
+    desc = ctx.attn_paged_desc(q, kc, vc, wide, i32(lens), out, max_len=max_len, recip_slot=RECIP_1_2, recip_pow2=True)
+    ctx.attention_pwl_paged(desc, torch.full((ctx.attention_paged_workspace_bytes(desc),), 255, dtype=torch.uint8, device="cuda"))
+    ctx.check_device_status()
+    scale = np.float64(np.float32(d ** -0.5))
+    for i, n in enumerate(lens):
+        ki, vi = f64(k[i])[:, 0], f64(v[i])[:, 0]
+        want, bound, soft, far = (np.zeros((hq, d)) for _ in range(4))
+        for h in range(hq if n else 0):
+            want[h], bound[h] = ref.attention(f64(q)[i, h], ki, vi, scale, ctx.tabs["exp"], tab, 0.0)
+            s = scale * (ki @ f64(q)[i, h])
+            p = np.exp(s - s.max())
+            p /= p.sum()
+            # secants of exp over 1/16 lie up to (1/16)^2 / 8 above it, of 1/x over 1/256 up to 2 (1/256)^2 / 8 above it; a weight's numerator and
+            # the sum both have the first
+            soft[h], far[h] = p @ vi, (2 * (1 / 16) ** 2 / 8 + 2 * (1 / 256) ** 2 / 8) * (p @ np.abs(vi))
+        check(out[i], want, bound, td, "request %d of %d tokens" % (i, n))
+        check(out[i], soft, bound + far, td, "softmax of %d tokens" % n)
+
+
+def test_attention_weights_add_up_to_one(nm, ctx):  # noqa: F811
+    """Values of one: what comes out is the sum of the weights, 1 with recip_pow2; with one table over all sums far from it."""
+    ctx.load_function_table(RECIP_1_2, nm.FUNC_RECIP, 256, 1.0, 2.0)
+    ctx.load_function_table(13, nm.FUNC_RECIP, 256, 32.0, 8193.0)
+    lens, hq, d = [1, 2, 16, 100, 1000, 8192], 4, 64
+    gen = gen_of(3)
+    kc, vc, tables, k, v = make_cache(gen, torch.float32, lens, 64, 2, d, "token")
+    vc.fill_(1.0)
+    q = randn(gen, len(lens), hq, d)
+    out = torch.empty_like(q)
+    for slot, pow2 in ((RECIP_1_2, True), (13, False)):
+        desc = ctx.attn_paged_desc(q, kc, vc, tables, i32(lens), out, max_len=8192, recip_slot=slot, recip_pow2=pow2)
+        ctx.attention_pwl_paged(desc, torch.empty(ctx.attention_paged_workspace_bytes(desc), dtype=torch.uint8, device="cuda"))
+        ctx.check_device_status()
+        off = (out.double() - 1).abs().amax((1, 2)).tolist()
+        if pow2:   # 2 (1/256)^2 / 8 of the table; two sums of n terms in some order of at most 300 steps each
+            assert max(off) <= 2 * (1 / 256) ** 2 / 8 + 600 * 2.0 ** -24, off
+        else:
+            assert off[0] > 0.9 and off[-1] < 0.1, off
