@@ -302,21 +302,52 @@ __global__ void __launch_bounds__(W4_THREADS, 2) linear_w4_kernel(const W4Args a
 #pragma unroll
                                     for (int i = 0; i < 4; ++i) part[r][n][i] = 0.f;
                         }
-#pragma unroll
-                        for (int r = 0; r < RW; ++r) {
+                        auto weights = [&](int r, uint32_t* lo, uint32_t* hi) {
                             const uint32_t w0 = *reinterpret_cast<const uint32_t*>(tile + (r * 16 + g) * 128 + ((j ^ g) << 4) + t * 4);
                             const uint32_t w1 = *reinterpret_cast<const uint32_t*>(tile + (r * 16 + g + 8) * 128 + ((j ^ g) << 4) + t * 4);
-                            uint32_t lo[4], hi[4];
                             w4_pairs(w0, lo, Mma());
                             w4_pairs(w1, hi, Mma());
+                        };
+                        if constexpr (TERMS == 1) {
 #pragma unroll
-                            for (int p = 0; p < 4; p += 2) {
-                                const uint32_t f[4] = {lo[p], hi[p], lo[p + 1], hi[p + 1]};
+                            for (int r = 0; r < RW; ++r) {
+                                uint32_t lo[4], hi[4];
+                                weights(r, lo, hi);
+#pragma unroll
+                                for (int p = 0; p < 4; p += 2) {
+                                    const uint32_t f[4] = {lo[p], hi[p], lo[p + 1], hi[p + 1]};
+#pragma unroll
+                                    for (int n = 0; n < NT; ++n) w4_mma(part[r][n], f, x[n][0][p], x[n][0][p + 1], Mma());
+                                }
+                            }
+                        } else {
+                            // The tensor core truncates its sums.  With three terms a group would be a chain of 6 to 24 products, whose
+                            // truncations show in fp32 (operands of one sign, K 128: 18 units of 2^-24 too little).  So the 32 k of a step have
+                            // a sum of their own, smallest terms first, and are added in fp32: two truncations count, half a unit in all.
+                            uint32_t lo[RW][4], hi[RW][4];
+                            float o[RW][NT][4];
+#pragma unroll
+                            for (int r = 0; r < RW; ++r) {
+                                weights(r, lo[r], hi[r]);
+#pragma unroll
+                                for (int n = 0; n < NT; ++n) o[r][n][0] = o[r][n][1] = o[r][n][2] = o[r][n][3] = 0.f;
+                            }
+#pragma unroll
+                            for (int s = TERMS - 1; s >= 0; --s)
+#pragma unroll
+                                for (int p = 0; p < 4; p += 2)
+#pragma unroll
+                                    for (int r = 0; r < RW; ++r) {
+                                        const uint32_t f[4] = {lo[r][p], hi[r][p], lo[r][p + 1], hi[r][p + 1]};
+#pragma unroll
+                                        for (int n = 0; n < NT; ++n) w4_mma(o[r][n], f, x[n][s][p], x[n][s][p + 1], Mma());
+                                    }
+#pragma unroll
+                            for (int r = 0; r < RW; ++r)
 #pragma unroll
                                 for (int n = 0; n < NT; ++n)
 #pragma unroll
-                                    for (int s = 0; s < TERMS; ++s) w4_mma(part[r][n], f, x[n][s][p], x[n][s][p + 1], Mma());
-                            }
+                                    for (int i = 0; i < 4; ++i) part[r][n][i] += o[r][n][i];
                         }
                         if (j % GS == GS - 1) {   // a group ends
                             const int gi = j / GS, from_lane = (lane & 28) | (gi & 3);
