@@ -106,14 +106,18 @@ class EncoderCfg(C.Structure):
                 ("recip_slot", C.c_int32), ("rsqrt_slot", C.c_int32), ("algo", C.c_int32)]
 
 
-class KvPlanDesc(C.Structure):
+class _Desc(C.Structure):
+    device = None   # index of the tensors' CUDA device (None: not known, as for fields that were set by hand)
+
+
+class KvPlanDesc(_Desc):
     _fields_ = [("B", C.c_int32), ("page_size", C.c_int32), ("max_pages", C.c_int32), ("max_tokens", C.c_int32),
                 ("free_capacity", C.c_int32), ("lengths", C.c_void_p), ("new_tokens", C.c_void_p), ("free_count", C.c_void_p),
                 ("block_tables", C.c_void_p), ("ld_tables", C.c_int64), ("free_pages", C.c_void_p), ("lengths_out", C.c_void_p),
                 ("free_count_out", C.c_void_p), ("token_start", C.c_void_p), ("slots", C.c_void_p), ("positions", C.c_void_p)]
 
 
-class QkRopeDesc(C.Structure):
+class QkRopeDesc(_Desc):
     _fields_ = [("T", C.c_int32), ("heads", C.c_int32), ("kv_heads", C.c_int32), ("d", C.c_int32), ("rot", C.c_int32),
                 ("pairs", C.c_int32), ("dtype", C.c_int), ("qkv", C.c_void_p), ("ld_qkv", C.c_int64), ("positions", C.c_void_p),
                 ("cos_sin", C.c_void_p), ("max_position", C.c_int32), ("gamma_q", C.c_void_p), ("gamma_k", C.c_void_p),
@@ -123,7 +127,7 @@ class QkRopeDesc(C.Structure):
                 ("stride_head", C.c_int64)]
 
 
-class AttnPagedDesc(C.Structure):
+class AttnPagedDesc(_Desc):
     _fields_ = [("B", C.c_int32), ("heads", C.c_int32), ("kv_heads", C.c_int32), ("d", C.c_int32), ("dtype", C.c_int),
                 ("num_pages", C.c_int32), ("page_size", C.c_int32), ("max_pages", C.c_int32), ("max_len", C.c_int32),
                 ("Q", C.c_void_p), ("ld_q", C.c_int64), ("k_cache", C.c_void_p), ("v_cache", C.c_void_p),
@@ -133,7 +137,7 @@ class AttnPagedDesc(C.Structure):
                 ("recip_pow2", C.c_int32)]
 
 
-class LinearW4Desc(C.Structure):
+class LinearW4Desc(_Desc):
     _fields_ = [("M", C.c_int64), ("N", C.c_int64), ("K", C.c_int64), ("dtype", C.c_int), ("group", C.c_int32), ("A", C.c_void_p),
                 ("lda", C.c_int64), ("codes", C.c_void_p), ("ld_codes", C.c_int64), ("scales", C.c_void_p), ("ld_scales", C.c_int64),
                 ("bias", C.c_void_p), ("residual", C.c_void_p), ("ldr", C.c_int64), ("slot", C.c_int32), ("out", C.c_void_p),
@@ -265,9 +269,12 @@ def _want(name, t, dtype, shape, inner=True):
 
 
 def _same_device(tensors):
-    seen = {str(t.device) for t in tensors if t is not None}
+    """The index of the CUDA device that all tensors are on (None: they are on the CPU)."""
+    seen = {t.device for t in tensors if t is not None}
     if len(seen) > 1:
-        raise ValueError("tensors on several devices: %s" % ", ".join(sorted(seen)))
+        raise ValueError("tensors on several devices: %s" % ", ".join(sorted(str(d) for d in seen)))
+    device = seen.pop() if seen else None
+    return device.index if device is not None and device.type == "cuda" else None
 
 
 def _pitch(t):
@@ -312,7 +319,7 @@ class Context:
         _check(self._lib.nm_ctx_create(C.byref(h), int(device)), "nm_ctx_create")
         self._h = h
         self._raw_stream = None
-        self.device = device
+        self.device = int(device)
 
     def close(self):
         if self._h:
@@ -481,10 +488,15 @@ class Context:
         d.B, d.page_size, d.max_pages = B, int(page_size), block_tables.shape[1]
         d.max_tokens, d.free_capacity, d.ld_tables = slots.shape[0], free_pages.shape[0], _pitch(block_tables) if B else d.max_pages
         d.tensors = [t for t, _ in one_dim.values()] + [block_tables]
-        _same_device(d.tensors)
+        d.device = _same_device(d.tensors)
         return d
 
+    def _on_this_device(self, desc):
+        if desc.device is not None and desc.device != self.device:
+            raise ValueError("the tensors are on device %d, the context on %d" % (desc.device, self.device))
+
     def kv_plan(self, desc, stream=None):
+        self._on_this_device(desc)
         _check(self._lib.nm_kv_plan(self._h, C.byref(desc), self._stream(stream)), "nm_kv_plan")
 
     @staticmethod
@@ -525,10 +537,11 @@ class Context:
             a.num_pages, a.page_size, (a.stride_page, a.stride_token, a.stride_head) = _cache_strides(k_cache, v_cache, qkv.dtype, kv_heads, d)
             a.k_cache, a.v_cache = k_cache.data_ptr(), v_cache.data_ptr()
         a.tensors = [qkv, q_out, positions, cos_sin, gamma_q, gamma_k, k_cache, v_cache, slots, k_out]
-        _same_device(a.tensors)
+        a.device = _same_device(a.tensors)
         return a
 
     def qk_norm_rope_pwl(self, desc, stream=None):
+        self._on_this_device(desc)
         _check(self._lib.nm_qk_norm_rope_pwl(self._h, C.byref(desc), self._stream(stream)), "nm_qk_norm_rope_pwl")
 
     @staticmethod
@@ -564,14 +577,19 @@ class Context:
         a.scale = float(scale) if scale is not None else float(d) ** -0.5
         a.exp_slot, a.recip_slot, a.recip_pow2 = exp_slot, recip_slot, 1 if recip_pow2 else 0
         a.tensors = [q, k_cache, v_cache, block_tables, lengths, out, token_start]
-        _same_device(a.tensors)
+        a.device = _same_device(a.tensors)
         return a
 
     def attention_paged_workspace_bytes(self, desc) -> int:
         return int(self._lib.nm_attention_paged_workspace_bytes(C.byref(desc)))
 
     def attention_pwl_paged(self, desc, workspace=None, stream=None):
-        ws = workspace.numel() * workspace.element_size() if workspace is not None else 0
+        self._on_this_device(desc)
+        ws = 0
+        if workspace is not None:
+            if workspace.get_device() != self.device or not workspace.is_contiguous():
+                raise ValueError("workspace: a contiguous tensor on the context's device is wanted")
+            ws = workspace.numel() * workspace.element_size()
         _check(self._lib.nm_attention_pwl_paged(self._h, C.byref(desc), _ptr(workspace), ws, self._stream(stream)), "nm_attention_pwl_paged")
 
     @staticmethod
@@ -598,10 +616,11 @@ class Context:
             a.residual, a.ldr = residual.data_ptr(), _pitch(residual)
         a.slot = slot
         a.tensors = [A, codes, scales, out, bias, residual]
-        _same_device(a.tensors)
+        a.device = _same_device(a.tensors)
         return a
 
     def linear_pwl_w4(self, desc, stream=None):
+        self._on_this_device(desc)
         _check(self._lib.nm_linear_pwl_w4(self._h, C.byref(desc), self._stream(stream)), "nm_linear_pwl_w4")
 
     # -- CNN ----------------------------------------------------------------------

@@ -54,3 +54,89 @@ def test_binding_of_the_rows_of_a_plan(lib):  # noqa: F811
                 {"out": z(2, 8, 64)}, {"block_tables": z(4, dtype=i)}, {"token_start": None}):
         with pytest.raises(ValueError):
             nm.Context.attn_paged_desc(**dict(good, **bad))
+
+
+# ---------------------------------------------------------------- what only the binding can see
+
+
+class FakeLibrary:
+    """Notes what would have been launched."""
+
+    def __init__(self):
+        self.calls = []
+
+    def __getattr__(self, name):
+        return lambda *a: self.calls.append(name) or 0
+
+
+@pytest.fixture
+def binding():
+    """A context of device 0 without a device, and the four calls with descriptors of tensors that lie nowhere."""
+    if torch.cuda.is_available():
+        pytest.skip("a machine without a device")
+    c = object.__new__(nm.Context)
+    c._lib, c._h, c._raw_stream, c.device = FakeLibrary(), None, lambda device: 0, 0
+    i = torch.int32
+    z = lambda *shape, dtype=torch.bfloat16: torch.zeros(shape, dtype=dtype)  # noqa: E731
+    cache, n = z(9, 16, 2, 64), z(2, dtype=i)
+    plan = c.kv_plan_desc(n, n, z(2, 4, dtype=i), z(9, dtype=i), z(1, dtype=i), 16, n, z(1, dtype=i), z(3, dtype=i), z(4, dtype=i), z(4, dtype=i))
+    calls = {"kv_plan": plan, "qk_norm_rope_pwl": c.qk_rope_desc(z(3, 512), 4, 2, 64, z(3, 256)),
+             "attention_pwl_paged": c.attn_paged_desc(z(2, 8, 64), cache, cache, z(2, 4, dtype=i), n, z(2, 8, 64)),
+             "linear_pwl_w4": c.linear_w4_desc(z(3, 128), z(24, 64, dtype=torch.uint8), z(24, 2), z(3, 24))}
+    return c, calls
+
+
+class Fake:
+    """As much of a tensor as a check of its place looks at."""
+
+    def __init__(self, device, size=1 << 20, contiguous=True):
+        self.device, self._size, self._contiguous = torch.device(device), size, contiguous
+
+    def get_device(self):
+        return -1 if self.device.type == "cpu" else self.device.index
+
+    def is_contiguous(self):
+        return self._contiguous
+
+    def numel(self):
+        return self._size
+
+    def element_size(self):
+        return 1
+
+    def data_ptr(self):
+        return A
+
+
+def test_descriptors_of_another_device_are_refused(binding):
+    c, calls = binding
+    for name, desc in calls.items():
+        for device in (1, 7):
+            desc.device = device
+            with pytest.raises(ValueError):
+                getattr(c, name)(desc)
+    assert not c._lib.calls
+    for name, desc in calls.items():
+        desc.device = 0
+        getattr(c, name)(desc)
+    assert c._lib.calls == ["nm_" + name for name in calls]
+
+
+def test_descriptors_know_their_device():
+    assert nm._same_device([None, Fake("cuda:1"), Fake("cuda:1")]) == 1 and nm._same_device([Fake("cuda:0")]) == 0
+    assert nm._same_device([Fake("cpu"), Fake("cpu")]) is None
+    with pytest.raises(ValueError):
+        nm._same_device([Fake("cuda:1"), Fake("cuda:0")])
+    with pytest.raises(ValueError):
+        nm._same_device([Fake("cuda:0"), Fake("cpu")])
+
+
+@pytest.mark.parametrize("workspace", [Fake("cpu"), Fake("cuda:1"), Fake("cuda:0", contiguous=False), torch.zeros(1 << 12, dtype=torch.uint8)])
+def test_workspaces_that_the_kernels_must_not_write_are_refused(binding, workspace):
+    c, calls = binding
+    with pytest.raises(ValueError):
+        c.attention_pwl_paged(calls["attention_pwl_paged"], workspace)
+    assert not c._lib.calls
+    c.attention_pwl_paged(calls["attention_pwl_paged"], Fake("cuda:0"))
+    c.attention_pwl_paged(calls["attention_pwl_paged"])
+    assert len(c._lib.calls) == 2
