@@ -286,10 +286,11 @@ def _cache_strides(k_cache, v_cache, dtype, kv_heads, d):
     """[num_pages, page_size, kv_heads, d] views of any strides with contiguous channels, K's and V's alike."""
     _want("k_cache", k_cache, dtype, (None, None, kv_heads, d))
     _want("v_cache", v_cache, dtype, tuple(k_cache.shape))
-    if k_cache.stride()[:3] != v_cache.stride()[:3]:
-        raise ValueError("k_cache and v_cache: the same strides are wanted, got %s and %s" % (k_cache.stride(), v_cache.stride()))
     # the stride of an extent of one is never used
-    return k_cache.shape[0], k_cache.shape[1], [s if n > 1 else 0 for s, n in zip(k_cache.stride()[:3], k_cache.shape[:3])]
+    strides, others = ([s if n > 1 else 0 for s, n in zip(t.stride()[:3], t.shape[:3])] for t in (k_cache, v_cache))
+    if strides != others:
+        raise ValueError("k_cache and v_cache: the same strides are wanted, got %s and %s" % (k_cache.stride(), v_cache.stride()))
+    return k_cache.shape[0], k_cache.shape[1], strides
 
 
 def pwl_table_build(func: int, n: int, x_min: float, x_max: float):

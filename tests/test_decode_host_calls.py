@@ -140,3 +140,18 @@ def test_workspaces_that_the_kernels_must_not_write_are_refused(binding, workspa
     c.attention_pwl_paged(calls["attention_pwl_paged"], Fake("cuda:0"))
     c.attention_pwl_paged(calls["attention_pwl_paged"])
     assert len(c._lib.calls) == 2
+
+
+def test_strides_of_extents_of_one_do_not_count(lib):  # noqa: F811
+    """With one key head (or one page, or pages of one token) the distance of heads is never used: K and V may differ in it."""
+    if torch.cuda.is_available():
+        pytest.skip("a machine without a device")
+    i = torch.int32
+    z = lambda *shape, dtype=torch.bfloat16: torch.zeros(shape, dtype=dtype)  # noqa: E731
+    k, v = z(9, 16, 1, 64), z(9, 1, 16, 64).transpose(1, 2)   # the same places, other strides of the one head
+    d = nm.Context.attn_paged_desc(z(2, 8, 64), k, v, z(2, 4, dtype=i), z(2, dtype=i), z(2, 8, 64))
+    assert (d.stride_page, d.stride_token, d.stride_head) == (1024, 64, 0)
+    d = nm.Context.qk_rope_desc(z(3, 384), 4, 1, 64, z(3, 256), k_cache=v, v_cache=k, slots=z(3, dtype=i))
+    assert (d.stride_page, d.stride_token, d.stride_head) == (1024, 64, 0)
+    with pytest.raises(ValueError):   # two heads: their distance counts
+        nm.Context.attn_paged_desc(z(2, 8, 64), z(9, 16, 2, 64), z(9, 2, 16, 64).transpose(1, 2), z(2, 4, dtype=i), z(2, dtype=i), z(2, 8, 64))
