@@ -109,6 +109,11 @@ class EncoderCfg(C.Structure):
 class _Desc(C.Structure):
     device = None   # index of the tensors' CUDA device (None: not known, as for fields that were set by hand)
 
+    def __setattr__(self, name, value):
+        if isinstance(value, int) and not -2 ** 31 <= value < 2 ** 31 and dict(self._fields_).get(name) is C.c_int32:
+            raise ValueError("%s: %d does not fit 32 bits" % (name, value))   # (ctypes would keep its lower bits)
+        super().__setattr__(name, value)
+
 
 class KvPlanDesc(_Desc):
     _fields_ = [("B", C.c_int32), ("page_size", C.c_int32), ("max_pages", C.c_int32), ("max_tokens", C.c_int32),

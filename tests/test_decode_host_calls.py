@@ -155,3 +155,25 @@ def test_strides_of_extents_of_one_do_not_count(lib):  # noqa: F811
     assert (d.stride_page, d.stride_token, d.stride_head) == (1024, 64, 0)
     with pytest.raises(ValueError):   # two heads: their distance counts
         nm.Context.attn_paged_desc(z(2, 8, 64), z(9, 16, 2, 64), z(9, 2, 16, 64).transpose(1, 2), z(2, 4, dtype=i), z(2, dtype=i), z(2, 8, 64))
+
+
+def test_numbers_that_do_not_fit_a_descriptor_are_refused(lib):  # noqa: F811
+    """32-bit fields would silently take a number's lower bits: pages of 2^32 + 16 tokens are no pages of 16."""
+    if torch.cuda.is_available():
+        pytest.skip("a machine without a device")
+    i, c = torch.int32, nm.Context
+    z = lambda *shape, dtype=torch.bfloat16: torch.zeros(shape, dtype=dtype)  # noqa: E731
+    n, cache = z(2, dtype=i), z(9, 16, 2, 64)
+    with pytest.raises(ValueError):
+        c.kv_plan_desc(n, n, z(2, 4, dtype=i), z(9, dtype=i), z(1, dtype=i), 2 ** 32 + 16, n, z(1, dtype=i), z(3, dtype=i), z(4, dtype=i), z(4, dtype=i))
+    good = (z(2, 8, 64), cache, cache, z(2, 4, dtype=i), n, z(2, 8, 64))
+    for bad in ({"max_len": 2 ** 32 + 8}, {"max_len": 2 ** 31}, {"max_len": -2 ** 31 - 1}, {"exp_slot": 2 ** 32 + nm.SLOT_EXP}, {"recip_slot": -2 ** 32}):
+        with pytest.raises(ValueError):
+            c.attn_paged_desc(*good, **bad)
+    long = torch.empty((1, 1 << 20), dtype=i)   # a table of 2^20 pages of 4096 tokens: 2^32
+    with pytest.raises(ValueError):
+        c.attn_paged_desc(z(1, 1, 8), z(1, 4096, 1, 8), z(1, 4096, 1, 8), long, n[:1], z(1, 1, 8))
+    d = c.attn_paged_desc(z(1, 1, 8), z(1, 4096, 1, 8), z(1, 4096, 1, 8), long, n[:1], z(1, 1, 8), max_len=4096)
+    assert d.max_len == 4096 and d.max_pages == 1 << 20
+    with pytest.raises(ValueError):
+        c.linear_w4_desc(z(3, 128), z(24, 64, dtype=torch.uint8), z(24, 2), z(3, 24), slot=2 ** 32)
