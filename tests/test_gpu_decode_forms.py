@@ -214,3 +214,102 @@ def test_attention_weights_add_up_to_one(nm, ctx):  # noqa: F811
             assert max(off) <= 2 * (1 / 256) ** 2 / 8 + 600 * 2.0 ** -24, off
         else:
             assert off[0] > 0.9 and off[-1] < 0.1, off
+
+
+# ---------------------------------------------------------------- equal shares of all tokens: what the one-launch form is tested for
+
+
+def shares(ctx, q, kc, vc, tables, lens, out=None, max_len=20000, **kw):  # noqa: F811
+    """The call with room for max_len tokens a request, so that blocks take equal shares; a workspace of NaN."""
+    wide = torch.full((len(lens), -(-max_len // kc.shape[1])), -5, dtype=torch.int32, device="cuda")
+    width = min(wide.shape[1], tables.shape[1])
+    wide[:, :width] = tables[:, :width]
+    out = torch.full_like(q, 5.0) if out is None else out
+    desc = ctx.attn_paged_desc(q, kc, vc, wide, i32(lens), out, max_len=max_len, **kw)
+    need = ctx.attention_paged_workspace_bytes(desc)
+    assert need > 0
+    ctx.attention_pwl_paged(desc, torch.full((need,), 255, dtype=torch.uint8, device="cuda"))
+    return out
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("hq,hk,d,layout", [(4, 2, 256, "token"), (9, 1, 256, "both"), (16, 1, 96, "head"), (16, 1, 128, "token"), (40, 2, 128, "token"),
+                                            (20, 1, 64, "both"), (6, 2, 200, "head"), (2, 1, 8, "token")])
+def test_attention_shares_of_every_core(ctx, dtype, hq, hk, d, layout):  # noqa: F811
+    """256 channels (one block an SM, two pieces a lane in fp32), 16 query heads a unit, odd head sizes."""
+    td, gen, lens = TYPES[dtype], gen_of(hq + d), [1700, 0, 33, 5003, 1]
+    kc, vc, tables, k, v = make_cache(gen, td, lens, 24, hk, d, layout)
+    q = randn(gen, len(lens), hq, d).to(td)
+    out = shares(ctx, q, kc, vc, tables, lens, max_len=100008 if d in (8, 200) else 20000)
+    ctx.check_device_status()
+    check_attention(ctx, q, k, v, out, lens, hq, hk, d, td)
+
+
+@pytest.mark.parametrize("dtype,hq,hk,d", [("bf16", 4, 1, 128), ("f16", 12, 1, 64), ("f32", 4, 2, 64)])
+def test_attention_shares_every_row_of_many(ctx, dtype, hq, hk, d):  # noqa: F811
+    td, gen = TYPES[dtype], gen_of(32)
+    lens = [int(n) for n in np.random.default_rng(6).integers(0, 161, 300)]
+    lens[0] = lens[17] = lens[18] = lens[299] = 0
+    lens[40], lens[41], lens[42] = 3001, 32, 31
+    kc, vc, tables, k, v = make_cache(gen, td, lens, 32, hk, d, "token")
+    q = randn(gen, 300, hq, d).to(td)
+    out = shares(ctx, q, kc, vc, tables, lens)
+    ctx.check_device_status()
+    check_attention(ctx, q, k, v, out, lens, hq, hk, d, td)
+
+
+@pytest.mark.parametrize("dtype,d", [("f32", 64), ("bf16", 128), ("f16", 64), ("bf16", 40)])
+@pytest.mark.parametrize("requests", [1, 3])   # with one request few units, joined by a third launch
+def test_attention_shares_nan_and_infinity_reach_their_heads_only(ctx, dtype, d, requests):  # noqa: F811
+    hq, hk, lens, td = 4, 2, [4000, 5000, 70][:requests], TYPES[dtype]
+    gen = gen_of(8)
+    kc, vc, tables, k, v = make_cache(gen, td, lens, 16, hk, d, "token")
+    vc[tables[0, 201].long(), 3, 0, 5] = float("inf")
+    kc[tables[requests - 1, 2].long(), 1, 1, 7] = float("nan")
+    q = randn(gen, requests, hq, d).to(td)
+    out = shares(ctx, q, kc, vc, tables, lens, max_len=100000)
+    ctx.check_device_status()
+    good = torch.isfinite(out)
+    assert not good[0, :2, 5].any() and good[0, :2].sum() == 2 * (d - 1)
+    assert not good[requests - 1, 2:].any()
+    if requests > 1:
+        assert good[0, 2:].all() and good[1].all() and good[2, :2].all()
+        check_attention(ctx, q[1:2], k[1:2], v[1:2], out[1:2], lens[1:2], hq, hk, d, td)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_attention_shares_offsets_beyond_31_bits(ctx, dtype):  # noqa: F811
+    """A cache of more than 2^31 elements, its last pages in use."""
+    hq, hk, d, page, td, n = 8, 8, 128, 128, TYPES[dtype], 300
+    pages = (1 << 31) // (page * hk * d) + 3
+    kc, vc = (torch.zeros((pages, page, hk, d), dtype=td, device="cuda") for _ in range(2))
+    gen = gen_of(5)
+    rows = [pages - 1, 0, pages - 2]
+    k, v = randn(gen, n, hk, d).to(td), randn(gen, n, hk, d).to(td)
+    for i, r in enumerate(rows):
+        m = min(page, n - i * page)
+        kc[r, :m], vc[r, :m] = k[i * page:i * page + m], v[i * page:i * page + m]
+    q = randn(gen, 1, hq, d).to(td)
+    out = shares(ctx, q, kc, vc, i32([rows]), [n])
+    ctx.check_device_status()
+    check_attention(ctx, q, [k], [v], out, [n], hq, hk, d, td)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("M", [3, 12, 32])
+def test_linear_w4_nan_reaches_its_token_and_all_of_it(ctx, dtype, M):  # noqa: F811
+    """A NaN times any code is NaN, of a code of zero too; the other tokens' sums are as without it."""
+    td, N, K = TYPES[dtype], 72, 512
+    gen = gen_of(M)
+    codes = torch.randint(0, 256, (N, K // 2), generator=gen, device="cuda", dtype=torch.uint8)
+    scales = torch.full((N, K // 128), 0.25, dtype=td, device="cuda")
+    a = randn(gen, M, K).to(td)
+    a[1, 301], a[M - 1, 5] = float("nan"), float("inf")
+    codes[:, 2] = 0x98                                     # the infinity meets a code of one (the high half), and its neighbour one of zero
+    out = torch.empty((M, N), dtype=td, device="cuda")
+    ctx.linear_pwl_w4(ctx.linear_w4_desc(a, codes, scales, out))
+    ctx.check_device_status()
+    assert torch.isnan(out[1]).all() and (out[M - 1] == float("inf")).all()
+    rest = [m for m in range(M) if m not in (1, M - 1)]
+    y, dy = ref.linear_w4(f64(a[rest]), codes.cpu().numpy(), f64(scales), None, None, None)
+    check(out[rest], y, dy, td)
