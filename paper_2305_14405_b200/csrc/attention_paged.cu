@@ -422,30 +422,33 @@ template <typename T, int D_, int NT> struct PagedMma {
                     look(n, i0 + PAGED_WARPS * TILE);
                     // The tensor core truncates its sums: a tile's products have a sum of their own, smallest terms first, and are added
                     // to those of the tiles before in fp32, rounded to nearest.  A product waits for the one before it, so with registers to
-                    // spare CHAINS sums go side by side (one row of 131071 tokens, fp16: 102 us with four, 111 with one).
-                    constexpr int CHAINS = NT > 1 ? 1 : D % 64 == 0 ? 4 : 3;
+                    // spare SIDE channel pieces go side by side, and the 16s of tokens apart (one row of 131071 tokens, fp16, 128 channels: 102 us
+                    // with four pieces, 111 with one; 64 requests of up to 4096 tokens, bf16, 64 channels: 66.2 us with the tokens apart, 67.6).
+                    constexpr int SIDE = NT > 1 ? 1 : D % 64 == 0 ? 4 : 3, APART = NT > 1 ? 1 : MT, SUMS = SIDE * APART;
 #pragma unroll
-                    for (int c0 = 0; c0 < D / 16; c0 += CHAINS) {
-                        float o[CHAINS][4];
+                    for (int c0 = 0; c0 < D / 16; c0 += SIDE) {
+                        float o[SUMS][4];
 #pragma unroll
-                        for (int c = 0; c < CHAINS; ++c) o[c][0] = o[c][1] = o[c][2] = o[c][3] = 0.f;
+                        for (int c = 0; c < SUMS; ++c) o[c][0] = o[c][1] = o[c][2] = o[c][3] = 0.f;
 #pragma unroll
                         for (int y = 0; y < 3; ++y) {
 #pragma unroll
                             for (int x = 0; x < MT; ++x)
 #pragma unroll
-                                for (int c = 0; c < CHAINS; ++c) paged_mma(o[c], v[x][c0 + c][0], v[x][c0 + c][1], v[x][c0 + c][2], v[x][c0 + c][3], w[y][x][0], w[y][x][1], T());
+                                for (int c = 0; c < SIDE; ++c)
+                                    paged_mma(o[x % APART * SIDE + c], v[x][c0 + c][0], v[x][c0 + c][1], v[x][c0 + c][2], v[x][c0 + c][3], w[y][x][0], w[y][x][1],
+                                              T());
                             if (Terms::LIFT != 1.f && y < 2) {
 #pragma unroll
-                                for (int c = 0; c < CHAINS; ++c)
+                                for (int c = 0; c < SUMS; ++c)
 #pragma unroll
                                     for (int r = 0; r < 4; ++r) o[c][r] *= 1.f / Terms::LIFT;
                             }
                         }
 #pragma unroll
-                        for (int c = 0; c < CHAINS; ++c)
+                        for (int c = 0; c < SIDE; ++c)
 #pragma unroll
-                            for (int r = 0; r < 4; ++r) acc[n][c0 + c][r] += o[c][r];
+                            for (int r = 0; r < 4; ++r) acc[n][c0 + c][r] += APART == 1 ? o[c][r] : o[c][r] + o[SUMS - SIDE + c][r];
                     }
                 }
             });
