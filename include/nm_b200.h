@@ -559,7 +559,8 @@ nm_status nm_qk_norm_rope_pwl(nm_ctx* ctx, const nm_qk_rope_desc* desc, void* st
  * best and up to 65504, and there an |e| below 2^-24 gives NaN with an infinite V).
  * heads a multiple of kv_heads; d a multiple of 8, at most 256.  Pointers 16-byte aligned, strides multiples of 16 bytes.
  * workspace: device, 256-byte aligned, nm_attention_paged_workspace_bytes of it (0 on a bad descriptor); calls that may be in
- * flight together, replays of captured graphs among them, need one each. */
+ * flight together, replays of captured graphs among them, need one each.  Where rows may be too long for a cluster it holds a score per
+ * request, head and token, 4 * B * heads * max_len bytes, whatever the requests' lengths: max_len should be what the calls need. */
 typedef struct {
     int32_t B, heads, kv_heads, d;
     nm_dtype dtype;

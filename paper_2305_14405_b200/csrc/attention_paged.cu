@@ -13,8 +13,9 @@
 //   PagedFma   fp32 and other d: FMAs, a few lanes per token
 // Partial sums are fp32 and are added in the order of warps and blocks: results do not depend on timing.
 // Measured: bf16, 48 requests of up to 8192 tokens, 8 key heads of 128 channels (697 MB) 129 us, 5.4 TB/s; one of 131071 tokens (537 MB)
-// 103 us, 5.2 TB/s; 12 heads of 64 over 500 tokens 5.4 us, the latency of a chain (pages, keys, maximum, values, sums) and a launch.
-// Of the long rows the scores kernel is near the bytes' time; the values kernel waits for it, and the sums' join, are the rest.
+// 103 us, 5.2 TB/s; 12 heads of 64 over 500 tokens 5.7 us, the latency of a chain (pages, keys, maximum, values, sums) and a launch.
+// Of the long rows the scores kernel is near the bytes' time; the values kernel waits for it, and the sums' join, are the rest.  In between
+// (10 to 150 MB) the fixed costs count most: 15 requests of up to 2898 tokens (95 MB) 32 us, one of 9000 with 4 key heads (18 MB) 20 us.
 #include "nm_common.cuh"
 
 namespace {
@@ -1189,12 +1190,12 @@ __global__ void __launch_bounds__(JOIN_THREADS) paged_join_kernel(const PagedArg
 
 // A segment costs a block some 4 us next to its bytes: the first pages and tokens to arrive, the warps' sums, the join.  So that blocks with
 // many short segments do not end last, each unit counts for as many bytes of K more as a block moves meanwhile.  bf16, 8 key heads of 128
-// channels, 64 requests of 1 to 4096 tokens: 0 / 32 / 64 / 96 / 128 / 256 KB 169 / 124 / 102 / 99 / 99 / 104 us; 15 requests of 0 to 2898
-// tokens 73 / 35 / 34 / 33 / 33 / 35 us; requests of 4096 tokens alike gain nothing.
+// channels, 64 requests of 1 to 4096 tokens: 0 / 32 / 64 / 96 / 128 / 256 KB 145 / 118 / 106 / 104 / 104 / 108 us; 15 requests of 0 to 2898
+// tokens 35 / 34 / 33 / 32 / 31 / 32 us; requests of 4096 tokens alike gain nothing.
 constexpr int PAGED_LEAD_BYTES = 96 * 1024;
 // Units up to which a third launch joins them: each lies in so many blocks that one block takes long to add them up, and waits for the
-// last of them first.  bf16, 128 channels, joined in the second launch against a third: 1 unit of 122567 tokens 58 against 33 us, 2 of 50000
-// 35 / 31, 4 of 50000 39 / 38, 8 of 65536 65 / 66, 256 of 4096 104 / 112.
+// last of them first.  bf16, 128 channels, joined in the second launch against a third: 1 unit of 122567 tokens 41 against 32 us, 2 of 50000
+// 32 / 28, 4 of 50000 35 / 35, 8 of 65536 60 / 62, 256 of 4096 102 / 110.
 constexpr int PAGED_JOIN_UNITS = 4;
 constexpr int PAGED_SMS = 148;   // the layout must not depend on the device: the workspace's size is asked for without one
 
@@ -1207,9 +1208,10 @@ int paged_heads(const nm_attn_paged_desc* d, bool mma)
 }
 // Tokens of a block of the fused form: scores take what rings of 64 KB leave of half an SM's shared memory.
 int paged_cap(int heads) { return (40 * 1024 - heads * 4 * 40) / (heads * 4) / 32 * 32; }
-// Bytes of K and V that a block of a cluster streams at most where the clusters leave SMs idle: split launches use all SMs at some 15 us more.
-// 128 channels, fused against split: bf16 4 key heads, 5000 / 9000 / 20000 tokens 12 / 17 / 29 against 19 / 20 / 29 us; fp32 5000 / 10000 /
-// 20000 tokens 21 / 38 / 68 against 19 / 24 / 29 us.  (Where none is idle: fp32, 16 requests of 4096 tokens, 8 key heads 88 against 102 us.)
+// Bytes of K and V that a block of a cluster streams at most where the clusters leave SMs idle: split launches use all SMs, and cost some 15 us
+// before the first byte.  One request, 4 key heads of 128 channels, fused against split: bf16, 5000 / 9000 tokens 14 / 20 against 18 / 20 us
+// (inputs in the L2: 13 / 18); fp32, 5000 / 10000 tokens 25 / 43 against 19 / 23 us, so for fp32 the border lies a little high when the cache is
+// cold (inputs in the L2: 21 against 19).
 int64_t paged_cluster_bytes(bool mma) { return mma ? 1280 * 1024 : 640 * 1024; }
 bool paged_mma_supported(const nm_attn_paged_desc* d) { return d->dtype != NM_F32 && (d->d == 64 || d->d == 96 || d->d == 128 || d->d == 256); }
 

@@ -4,11 +4,14 @@
 // tokens, nothing padded but the last tokens), their codes made 16-bit numbers in registers: a word of eight codes gives pairs
 // (k, k + 4) by one mask each, 128 + c (bf16) or 1024 + c (fp16) by the bits, c - 8 by one exact subtraction, so products and their
 // sums within a group are those of whole numbers and activations; the group's sum takes its scale in fp32.  tcgen05 would want the
-// 16-bit weights written to tensor or shared memory first, four times the bytes that arrive, and a drain per group.
-// Measured, bf16, 16384 x 8192 (67 MB of codes: 10.3 us; the copies alone take 14.5 us): 1 token 31 us, 8 tokens 32 us, 32 tokens 53 us.
-// Up to 8 tokens the chain from a code's word to its product bounds it, more warps in flight did not help; at 32 tokens instructions
-// (0.46 per cycle and scheduler, tensor pipe 30 % busy) and 256 blocks on 148 SMs.
-// fp32 activations are three bf16 terms (8 + 8 + 8 bits: exact), three products each.
+// 16-bit weights written to tensor or shared memory first, four times the bytes that arrive, and the accumulator read back per group; for
+// many tokens that would pay (weights are unpacked again for every 32 here), and is not built.
+// Measured, bf16, 16384 x 8192 (67 MB of codes: 10.3 us; the copies alone take 14.5 us): 1 token 30 us, 8 tokens 32 us, 32 tokens 52 us,
+// 512 tokens 643 us.  Up to 8 tokens the streams are short: 512 blocks on 296 places, four blocks of k a warp for a ring of three stages, so
+// rings that fill and drain, sums that are joined and the second wave are most of it.  At 32 tokens fragments from shared memory (2 KB for 256
+// bytes of codes), instructions (0.46 per cycle and scheduler, tensor pipe 30 % busy) and 256 blocks on 148 SMs.
+// fp32 activations are three bf16 terms (8 + 8 + 8 bits: exact), three products each: 1 / 8 / 16 / 32 tokens 59 / 64 / 118 / 188 us; above 8
+// tokens the shared fragments leave one block an SM.
 //
 // Every warp streams its own weights through a ring of asynchronous copies (256 codes of 16 or 32 rows a stage, so 128 bytes a row):
 // no barrier in the loop.  Activations come through L1, shared by the warps of a block that work on the same k.

@@ -827,8 +827,11 @@ size_t nm_attention_paged_bytes(const nm_attn_paged_desc* d);   // of a checked 
 nm_status nm_launch_attention_paged(nm_ctx* ctx, const nm_attn_paged_desc* d, void* workspace, cudaStream_t st);
 nm_status nm_launch_linear_w4(nm_ctx* ctx, const nm_linear_w4_desc* d, cudaStream_t st);
 
-// launch attributes of a kernel that may start while its predecessor runs (every thread of it calls nm_grid_dependency_wait
-// before it touches memory)
+// Launch attributes of a kernel that may start while its predecessor runs.  Every thread of it calls nm_grid_dependency_wait, before which
+// it writes no global memory and reads only what no kernel of a stream writes (the tables).  The one exception, the values kernel of the
+// paged attention, reads the call's inputs before its wait: the launch before it is the same call's, and triggers
+// (nm_grid_launch_dependents) only after its own wait, when everything before the call is complete.  A kernel whose successor does so
+// must not trigger earlier.
 struct NmLaunchConfig {
     cudaLaunchConfig_t cfg;
     cudaLaunchAttribute attr[2];

@@ -1,8 +1,10 @@
 // Norm of the heads of queries and keys (PWL rsqrt), rotation by position and write to the paged cache: one pass over the
 // packed projection.  Each element is read once and written once, rounded once at the end; sums and rotation are fp32.
-// Measured: 16383 tokens of 48 heads of 128 in bf16 (407 MB) 87 us, 4.7 TB/s; 192 tokens 4.2 us; one token 3.3 us, all of it latency.
-// The large case is bound by issue: about 0.57 instructions per cycle and scheduler with half of the DRAM rate taken; without norm and
-// rotation the same moves take 70 to 75 us.
+// Measured: 16383 tokens of 48 heads of 128 in bf16 (407 MB), half of the channels turned in neighbouring pairs 87 us, 4.7 TB/s, all of them
+// turned in halves 101 us; 192 tokens 4.4 us; one token 3.0 us, all of it latency.
+// Large cases issue about 0.57 instructions per cycle and scheduler with half of the DRAM rate taken: the partner's piece is read and widened a second
+// time when halves turn, values pass through registers, and where a group holds more heads than there are key heads its lanes idle (9899
+// tokens of 8 + 2 heads of 128: 32 us for 10 of bytes).  Without norm and rotation the same moves take 70 to 75 us.
 // A warp goes through its units (a token, a few of its heads) with the next ones' elements on their way to a ring in shared memory; a
 // lane copies what it will read itself, so there is no barrier.
 #include <type_traits>
